@@ -472,6 +472,103 @@ dppo_status dppo_scale_dlogits(const void* dlogits, int32_t dtype, int64_t T, in
                                const float* g, void* out, void* stream);
 dppo_status dppo_scale_to_bf16(const float* src, int64_t n, const float* g, void* dst, void* stream);
 
+/* Most entries of a teacher's record, and most candidates top_logits returns for a row. */
+#define DPPO_MAX_TOP 256
+
+/*
+ * top_logits -- the k largest logits of every row, best first, with the row's log-sum-exp: a
+ * teacher's record for distill_loss_fwd_bwd, or a step's candidates.
+ *
+ *  logits       as for logprob_fwd; V <= 2^28.
+ *  k            1 <= k <= min(V, DPPO_MAX_TOP).
+ *  temperature  tau > 0, finite, with 1 / tau finite.
+ *  values_out   [T, k] float32, the logits themselves (not divided by tau; -0 is returned as 0).
+ *  ids_out      [T, k] int32, their places. Equal values come lowest id first; a NaN counts as
+ *               larger than every number.
+ *  lse_out      [T] float32: log sum_v exp(z[t, v] / tau) over the whole row, non-finite rows as
+ *               in logprob_fwd.
+ *  workspace    device buffer of top_logits_workspace_bytes bytes or more, 16-byte aligned; scratch.
+ *               0 bytes (NULL allowed) unless few long rows are cut into parts.
+ * T = 0 enqueues nothing.
+ */
+dppo_status top_logits(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld, int32_t k,
+                       double temperature, float* values_out, int32_t* ids_out, float* lse_out,
+                       void* workspace, int64_t workspace_bytes, void* stream);
+/* Workspace bytes of such a call (-1 if the sizes are out of range). */
+int64_t top_logits_workspace_bytes(int32_t dtype, int64_t T, int64_t V, int32_t k);
+
+/*
+ * distill_loss_fwd_bwd -- distillation from a teacher's top logits: per token the divergence of
+ * the student's softmax q = softmax(z / tau) from the teacher's record, and its gradient.
+ * Row t's record is k values (teacher logits) with their token ids; p_j are its probabilities:
+ *    teacher_lse NULL:  p = softmax(values / tau) over the record;
+ *    teacher_lse given: p_j = exp(values_j / tau - teacher_lse), teacher_lse being the teacher's
+ *                       log-sum-exp at tau (top_logits' lse_out); what the record leaves out, Pt =
+ *                       max(0, 1 - sum p), is one more outcome, to which the student gives the mass
+ *                       Qt outside the record (at least 2^-24).
+ *    l_t = sum_j p_j (log p_j - log q[id_j])  (+ Pt log(Pt / Qt) with teacher_lse)
+ *    L = sum_t m_t s_t l_t, s_t as in decoupled_ppo_loss_fwd_bwd
+ *    dlogits[t, v] = m_t s_t dl_t / dz[t, v]:
+ *       outside the record  (s / tau) q_v (P - Pt Q / Qt),  P = sum p, Q = sum_record q,
+ *       inside it           (s / tau) (q_v (P + Pt) - p_v),  with Pt = 0 without teacher_lse.
+ * p_j = 0 (a value of -inf) contributes 0. A token that stands in the record twice counts as two
+ * entries: each has its term of l, and its gradient subtracts both probabilities.
+ *
+ *  logits, dlogits  as in decoupled_ppo_loss_fwd_bwd (dlogits NULL: no gradient); V <= 2^28.
+ *  teacher_values   [T, k] float32.   teacher_ids [T, k] int32; -1 marks an empty entry (a record
+ *                   shorter than k), whose value is not used. 1 <= k <= DPPO_MAX_TOP.
+ *  teacher_lse      [T] float32 or NULL.
+ *  loss_mask, token_scale, scale_mode, loss_scale  as in decoupled_ppo_loss_fwd_bwd.
+ *  temperature      tau > 0, finite, with 1 / tau finite.
+ *  kl_out           [T] float32: l_t (0 on masked and bad rows).
+ *  loss_out         [1] float32, summed as in decoupled_ppo_loss_fwd_bwd.
+ *  flags_out        [T] uint8: DPPO_FLAG_VALID, DPPO_FLAG_BAD_ID.
+ *  stats_out        [5] int32: DPPO_STAT_N_VALID and DPPO_STAT_N_BAD; the others are 0.
+ * Rows with m_t = 0 are not read. A row whose record holds an id below -1 or past V - 1 is bad:
+ * l_t = 0, a zero dlogits row. A row whose record is empty has l_t = 0 and a zero dlogits row, up to
+ * its rounding with teacher_lse. Non-finite logits, values and teacher_lse follow IEEE arithmetic.
+ */
+dppo_status distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
+                                 const float* teacher_values, const int32_t* teacher_ids, int32_t k,
+                                 const float* teacher_lse, const uint8_t* loss_mask,
+                                 const float* token_scale, double temperature, int32_t scale_mode,
+                                 float loss_scale, float* kl_out, float* loss_out, uint8_t* flags_out,
+                                 int32_t* stats_out, void* dlogits, int64_t ld_dlogits, void* stream);
+
+/*
+ * verify_drafts -- speculative decoding's check of drafted tokens against the policy, with the
+ * caller's random numbers, so that the emitted tokens are distributed as the policy's own samples.
+ * For sequence b with n = num_drafts[b] drafts x_0 .. x_{n-1}, p_i = softmax(target[b, i] / tau),
+ * q_i = softmax(draft[b, i] / tau):
+ *   draft i is accepted while accept_u[b, i] q_i(x_i) < p_i(x_i); let a be the first that is not,
+ *   or n. Then one token is drawn: from max(p_a - q_a, 0) normalised if a < n, from p_n if a = n.
+ *   The draw is by inversion: the lowest v with sum_{w <= v} r_w > sample_u[b] sum r (if rounding or
+ *   sample_u >= 1 leave none, the last v with r_v > 0; if all r are 0, r = p_a).
+ *
+ *  target      [B, D + 1, V] of `dtype`: row i of sequence b at target + b * target_seq + i *
+ *              target_row (elements), row i the policy's logits behind draft i - 1.
+ *  draft       [B, D, V] of `dtype` with strides draft_seq, draft_row: the draft model's logits; NULL:
+ *              drafts without a distribution (greedy, n-gram), q_i = 1 at x_i and 0 elsewhere.
+ *  draft_ids   [B, D] int64.   num_drafts [B] int32 or NULL (all D); values are held in [0, D].
+ *  accept_u    [B, D] float32, sample_u [B] float32, in [0, 1).
+ *  B >= 0, 0 <= D <= 1024 (accept_u and draft_ids may be NULL with D = 0), 1 <= V <= 2^28.
+ *  accepted_out [B] int32: a.
+ *  tokens_out   [B, D + 1] int64: the accepted drafts, the drawn token, then -1.
+ *  logp_out     [B, D + 1] float32: log p_i of the emitted tokens (log mu_old of the loss calls), then 0.
+ *  workspace    device buffer of verify_drafts_workspace_bytes bytes or more, 16-byte aligned.
+ * The decisions and the draw are computed in 64 bits. Rows behind a are not part of the result. A
+ * sequence that reaches a draft id outside [0, V), or a row holding NaN or +inf or only -inf, ends
+ * there: its drawn token is -1, with log-prob NaN.
+ */
+dppo_status verify_drafts(const void* target, int64_t target_seq, int64_t target_row, const void* draft,
+                          int64_t draft_seq, int64_t draft_row, int32_t dtype, int64_t B, int64_t D,
+                          int64_t V, const int64_t* draft_ids, const int32_t* num_drafts,
+                          const float* accept_u, const float* sample_u, double temperature,
+                          int32_t* accepted_out, int64_t* tokens_out, float* logp_out, void* workspace,
+                          int64_t workspace_bytes, void* stream);
+/* Workspace bytes of such a call (-1 if the sizes are out of range). with_draft: draft is given. */
+int64_t verify_drafts_workspace_bytes(int32_t dtype, int64_t B, int64_t D, int64_t V, int32_t with_draft);
+
 /* Row-kernel policy, a testing and benchmarking hook, two bits. Bit 0: clear = automatic
  * (the register-resident kernel when the row fits, the two-pass streaming kernel
  * otherwise), set = always the streaming kernel. Bit 1: decoupled_ppo_loss_fwd_bwd counts

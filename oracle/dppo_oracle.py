@@ -558,3 +558,133 @@ def versioned_logprob(logits_by_version, version, ids):
             lp, _ = logprob_fwd(as_f64(np.asarray(z)[rows]), ids[rows])
             out[rows] = lp
     return out
+
+
+# ---------------------------------------------------------------------------------------------
+# Teacher records, distillation and draft verification: row by row, in float64.
+# ---------------------------------------------------------------------------------------------
+def top_logits(z, k, tau=1.0):
+    """(values, ids, lse): the k largest entries of every row, best first, equal values by their
+    index, NaN above every number; lse of z / tau (NaN for rows holding NaN or +inf, or only -inf)."""
+    z = as_f64(z)
+    T, V = z.shape
+    ids = np.empty((T, k), dtype=np.int64)
+    for t in range(T):
+        rank = np.where(np.isnan(z[t]), np.inf, z[t])
+        order = np.lexsort((np.arange(V), -rank, ~np.isnan(z[t])))
+        ids[t] = order[:k]
+    with np.errstate(invalid="ignore"):
+        lse = row_logsumexp(z / tau)
+    return np.take_along_axis(z, ids, axis=1), ids, lse
+
+
+DISTILL_TAIL_FLOOR = 2.0 ** -24
+
+
+def distill_loss(z, values, ids, lse=None, mask=None, token_scale=None, tau=1.0,
+                 scale_mode="token_mean", loss_scale=1.0):
+    """dict(kl, loss, flags, n_valid, n_bad, dlogits, slack): slack bounds, per dlogits entry, the
+    sizes of the terms it is the difference of."""
+    z, values = as_f64(z), as_f64(values)
+    ids = np.asarray(ids).astype(np.int64)
+    T, V = z.shape
+    m = np.ones(T, dtype=np.uint8) if mask is None else np.asarray(mask)
+    ts = np.ones(T) if token_scale is None else np.asarray(token_scale, dtype=np.float64)
+    n_valid = int((m != 0).sum())
+    scale = loss_scale / max(1, n_valid) if scale_mode == "token_mean" else loss_scale
+    kl, flags = np.zeros(T), np.zeros(T, dtype=np.uint8)
+    d, slack = np.zeros((T, V)), np.zeros((T, V))
+    loss = 0.0
+    for t in range(T):
+        if not m[t]:
+            continue
+        flags[t] = FLAG_VALID
+        if ((ids[t] < -1) | (ids[t] >= V)).any():
+            flags[t] |= FLAG_BAD_ID
+            continue
+        with np.errstate(all="ignore"):
+            x = z[t] / tau
+            norm = row_logsumexp(x[None])[0]
+            logq = x - norm
+            q = np.exp(logq)
+            entries = [j for j in range(ids.shape[1]) if ids[t, j] >= 0]
+            tt = values[t, entries] / tau
+            if lse is None:
+                c = row_logsumexp(tt[None])[0] if len(tt) and not np.all(tt == -np.inf) else 0.0
+            else:
+                c = float(lse[t])
+            logp = tt - c
+            p = np.exp(logp)
+            tok = ids[t, entries]
+            terms = np.where(p == 0, 0.0, p * (logp - logq[tok]))
+            l, P = terms.sum(), p.sum()
+            inside = np.zeros(V, dtype=bool)
+            inside[tok] = True
+            f = g = fs = P
+            if lse is not None:
+                Q = q[inside].sum()
+                Pt = max(1.0 - P, 0.0)
+                Qt = max(q[~inside].sum(), DISTILL_TAIL_FLOOR)
+                if Pt > 0:
+                    l += Pt * np.log(Pt / Qt)
+                f, g, fs = P - Pt * Q / Qt, P + Pt, P + Pt * Q / Qt
+            s = scale * ts[t] / tau
+            row = s * np.where(inside, g, f) * q
+            size = np.abs(s) * np.where(inside, g, fs) * q
+            for j, v in enumerate(tok):
+                row[v] -= s * p[j]
+                size[v] += abs(s) * p[j]
+            kl[t], d[t], slack[t] = l, row, size
+            loss += scale * ts[t] * l
+    return dict(kl=kl, loss=loss, flags=flags, n_valid=n_valid, n_bad=int((flags & FLAG_BAD_ID != 0).sum()),
+                dlogits=d, slack=slack)
+
+
+def log_softmax_row(x):
+    """x - log sum exp x, the maximum taken off first (a row of far values keeps its shape)."""
+    x = x - x.max()
+    return x - np.log(np.exp(x).sum())
+
+
+def verify_drafts(target, draft_ids, accept_u, sample_u, draft=None, num=None, tau=1.0):
+    """(accepted [B], tokens [B, D + 1], logp [B, D + 1]) of speculative decoding's check."""
+    target = as_f64(target)
+    B, D1, V = target.shape
+    D = D1 - 1
+    draft = None if draft is None else as_f64(draft)
+    acc = np.zeros(B, dtype=np.int64)
+    tokens = np.full((B, D1), -1, dtype=np.int64)
+    logp = np.zeros((B, D1))
+    for b in range(B):
+        n = D if num is None else min(max(int(num[b]), 0), D)
+        for i in range(n + 1):
+            acc[b] = i
+            with np.errstate(all="ignore"):
+                lp = log_softmax_row(target[b, i] / tau)
+                r = np.exp(lp)
+                bad = bool(np.isnan(lp).any())
+                if i < n:
+                    y = int(draft_ids[b, i])
+                    bad = bad or not 0 <= y < V
+                    if not bad:
+                        if draft is None:
+                            q = np.zeros(V)
+                            q[y] = 1.0
+                        else:
+                            q = np.exp(log_softmax_row(draft[b, i] / tau))
+                            bad = bool(np.isnan(q).any())
+            if bad:
+                logp[b, i] = np.nan
+                break
+            if i < n:
+                if float(accept_u[b, i]) * q[y] < r[y]:
+                    tokens[b, i], logp[b, i] = y, lp[y]
+                    continue
+                rest = np.maximum(r - q, 0.0)
+                r = rest if rest.sum() > 0 else r
+            c = np.cumsum(r)
+            over = np.nonzero((c > float(sample_u[b]) * c[-1]) & (r > 0))[0]
+            v = over[0] if len(over) else np.nonzero(r > 0)[0][-1]
+            tokens[b, i], logp[b, i] = v, lp[v]
+            break
+    return acc, tokens, logp

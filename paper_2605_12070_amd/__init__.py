@@ -29,6 +29,8 @@ __all__ = [
     "fused_lm_head_loss_fwd_bwd_noalloc",
     "logprob_fwd_versioned", "EwmaProxyDevice", "vocab_shard_stats", "vocab_shard_combine",
     "decoupled_ppo_loss_shard_fwd_bwd", "FusedLMHeadLoss",
+    "top_logits", "TopLogits", "distill_loss_fwd_bwd", "DistillResult", "DistillLoss",
+    "verify_drafts", "VerifyResult",
 ]
 
 
@@ -627,6 +629,22 @@ def _same_rows(rows, d: torch.Tensor) -> bool:
             and f.is_contiguous() and lt.is_contiguous())
 
 
+def _scaled_dlogits(d, g_loss, rows, rd_mode: int):
+    """g_loss * dlogits in one pass. rows: the forward's flags and per-token losses, by which the
+    rows that are zero are not read, or ()."""
+    if d.dim() == 2 and d.dtype in (torch.bfloat16, torch.float32) and _scalable(d, g_loss, d.dtype):
+        T, V = d.shape
+        flags, loss_tok = rows if _same_rows(rows, d) else (None, None)
+        out = torch.empty_like(d)
+        st = _lib.lib().dppo_scale_dlogits(
+            d.data_ptr(), _dtype_code(d), T, V, flags.data_ptr() if flags is not None else None,
+            loss_tok.data_ptr() if loss_tok is not None else None, rd_mode, g_loss.data_ptr(),
+            out.data_ptr(), _stream(d.device))
+        _lib.check(st, "dppo_scale_dlogits")
+        return out
+    return d * g_loss.to(d.dtype)
+
+
 class DecoupledPPOLoss(torch.autograd.Function):
     """Autograd wrapper: forward runs the fused kernel (loss and dlogits at once); backward
     returns grad_output * dlogits in one pass, which does not read the rows that the forward's
@@ -652,17 +670,7 @@ class DecoupledPPOLoss(torch.autograd.Function):
         d, *rows = ctx.saved_tensors
         if g_loss is None:
             g_loss = torch.zeros((), dtype=torch.float32, device=d.device)
-        if d.dim() == 2 and d.dtype in (torch.bfloat16, torch.float32) and _scalable(d, g_loss, d.dtype):
-            T, V = d.shape
-            flags, loss_tok = rows if _same_rows(rows, d) else (None, None)
-            out = torch.empty_like(d)
-            st = _lib.lib().dppo_scale_dlogits(
-                d.data_ptr(), _dtype_code(d), T, V, flags.data_ptr() if flags is not None else None,
-                loss_tok.data_ptr() if loss_tok is not None else None, RD_MODES[ctx.rd_mode],
-                g_loss.data_ptr(), out.data_ptr(), _stream(d.device))
-            _lib.check(st, "dppo_scale_dlogits")
-        else:
-            out = d * g_loss.to(d.dtype)
+        out = _scaled_dlogits(d, g_loss, rows, RD_MODES[ctx.rd_mode])
         return (out, None, None, None, None, None, None, None)
 
 
@@ -704,3 +712,187 @@ class FusedLMHeadLoss(torch.autograd.Function):
         gw = FusedLMHeadLoss._scaled(dw, g_loss, tw) if ctx.needs_input_grad[1] else None
         return (gh, gw, None, None, None, None, None, None, None)
 
+
+# ------------------------------------------------------------------ teacher records and drafts
+def _plain(t: torch.Tensor, name: str):
+    """The tensor itself, refused where its memory holds something else than its values."""
+    if t.is_neg():
+        raise ValueError(f"{name} must not be a lazily negated view")
+    return t
+
+
+def _tensor(t, shape, dtype, name, dev):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not _plain(t, name).is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} {dtype} tensor")
+    if t.device != dev:
+        raise ValueError(f"{name} must live on {dev}")
+    return t.data_ptr()
+
+
+class _on_device:
+    """The tensors' device as the current one while a call launches on it."""
+
+    def __init__(self, dev):
+        self.want = dev.index
+
+    def __enter__(self):
+        self.old = torch._C._cuda_getDevice()
+        if self.old != self.want:
+            torch.cuda.set_device(self.want)
+
+    def __exit__(self, *exc):
+        if self.old != self.want:
+            torch.cuda.set_device(self.old)
+
+
+@dataclass
+class TopLogits:
+    values: torch.Tensor        # [T, k] fp32, best first
+    ids: torch.Tensor           # [T, k] int32
+    lse: torch.Tensor           # [T] fp32: log-sum-exp of the whole row at the temperature
+
+
+def top_logits(logits: torch.Tensor, k: int, *, temperature: float = 1.0) -> TopLogits:
+    """The k largest logits of every row of logits [T, V] (bf16 or fp32), best first (equal values:
+    lowest id first), and the rows' log-sum-exps of logits / temperature: a teacher's record for
+    distill_loss_fwd_bwd, or a step's candidates. 1 <= k <= min(V, 256)."""
+    ptr, T, V, ld = _matrix(_plain(logits, "logits"), "logits")
+    dev = logits.device
+    code = _dtype_code(logits)
+    n = _lib.lib().top_logits_workspace_bytes(code, T, V, int(k))
+    k = int(k)
+    rows = max(k, 0) if n >= 0 else 0          # sizes out of range: the call says which
+    values = torch.empty(T, rows, dtype=torch.float32, device=dev)
+    ids = torch.empty(T, rows, dtype=torch.int32, device=dev)
+    lse = torch.empty(T, dtype=torch.float32, device=dev)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n > 0 else None
+    with _on_device(dev):
+        st = _lib.lib().top_logits(ptr, code, T, V, ld, k, float(temperature), values.data_ptr(),
+                                   ids.data_ptr(), lse.data_ptr(),
+                                   ws.data_ptr() if ws is not None else None, max(n, 0), _stream(dev))
+    _lib.check(st, "top_logits")
+    return TopLogits(values, ids, lse)
+
+
+@dataclass
+class DistillResult:
+    loss: torch.Tensor          # [1] fp32: sum_t m_t s_t l_t
+    kl: torch.Tensor            # [T] fp32: l_t
+    flags: torch.Tensor         # [T] uint8: FLAG_VALID, FLAG_BAD_ID
+    stats: torch.Tensor         # [5] int32: STAT_N_VALID, STAT_N_BAD
+    dlogits: torch.Tensor | None
+
+
+def distill_loss_fwd_bwd(logits, teacher_values, teacher_ids, teacher_lse=None, loss_mask=None,
+                         token_scale=None, *, temperature=1.0, scale_mode="token_mean",
+                         loss_scale=1.0, want_dlogits=True, dlogits=None) -> DistillResult:
+    """Distillation from a teacher's top logits: per token the divergence of softmax(logits /
+    temperature) from the record teacher_values [T, k] fp32, teacher_ids [T, k] int32 (-1: an empty
+    entry), and its gradient. Without teacher_lse the record is renormalised; with it (top_logits'
+    lse, at the same temperature) what the record leaves out is one more outcome. The loss is
+    scaled as decoupled_ppo_loss_fwd_bwd scales its own (a temperature's square, where wanted, goes
+    into loss_scale). `dlogits` may be the logits tensor itself."""
+    ptr, T, V, ld = _matrix(_plain(logits, "logits"), "logits")
+    dev = logits.device
+    if teacher_values.dim() != 2:
+        raise ValueError("teacher_values must be a [T, k] tensor")
+    k = teacher_values.shape[1]
+    tv = _tensor(teacher_values, (T, k), torch.float32, "teacher_values", dev)
+    ti = _tensor(teacher_ids, (T, k), torch.int32, "teacher_ids", dev)
+    tl = None if teacher_lse is None else _tensor(teacher_lse, (T,), torch.float32, "teacher_lse", dev)
+    msk = _vec(loss_mask, T, torch.uint8, "loss_mask", dev, optional=True)
+    tsc = None if token_scale is None else _tensor(token_scale, (T,), torch.float32, "token_scale", dev)
+    if scale_mode not in SCALE_MODES:
+        raise ValueError(f"scale_mode in {list(SCALE_MODES)}")
+    f32 = dict(dtype=torch.float32, device=dev)
+    out = DistillResult(loss=torch.empty(1, **f32), kl=torch.empty(T, **f32),
+                        flags=torch.empty(T, dtype=torch.uint8, device=dev),
+                        stats=torch.empty(_lib.N_STATS, dtype=torch.int32, device=dev), dlogits=None)
+    d_ptr, ldd = None, 0
+    if want_dlogits:
+        if dlogits is None:
+            dlogits = torch.empty_like(logits)
+        if (dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.stride(1) != 1
+                or dlogits.device != dev):
+            raise ValueError("dlogits must match logits in dtype, shape and device, unit last stride")
+        out.dlogits = _plain(dlogits, "dlogits")
+        d_ptr, ldd = dlogits.data_ptr(), dlogits.stride(0)
+    with _on_device(dev):
+        st = _lib.lib().distill_loss_fwd_bwd(
+            ptr, _dtype_code(logits), T, V, ld, tv, ti, k, tl, msk, tsc, float(temperature),
+            SCALE_MODES[scale_mode], float(loss_scale), out.kl.data_ptr(), out.loss.data_ptr(),
+            out.flags.data_ptr(), out.stats.data_ptr(), d_ptr, ldd, _stream(dev))
+    _lib.check(st, "distill_loss_fwd_bwd")
+    return out
+
+
+class DistillLoss(torch.autograd.Function):
+    """Autograd wrapper: forward runs distill_loss_fwd_bwd (loss and dlogits at once); backward
+    returns grad_output * dlogits in one pass. The teacher's record gets no gradient."""
+
+    @staticmethod
+    def forward(ctx, logits, teacher_values, teacher_ids, teacher_lse, loss_mask, token_scale, kwargs):
+        res = distill_loss_fwd_bwd(logits, teacher_values, teacher_ids, teacher_lse, loss_mask,
+                                   token_scale, **(kwargs or {}))
+        ctx.save_for_backward(res.dlogits)
+        ctx.set_materialize_grads(False)     # no zero fills for kl and stats
+        ctx.mark_non_differentiable(res.kl, res.stats)
+        return res.loss[0], res.kl, res.stats
+
+    @staticmethod
+    def backward(ctx, g_loss, g_kl, g_stats):
+        (d,) = ctx.saved_tensors
+        if g_loss is None:
+            g_loss = torch.zeros((), dtype=torch.float32, device=d.device)
+        return (_scaled_dlogits(d, g_loss, (), 0), None, None, None, None, None, None)
+
+
+@dataclass
+class VerifyResult:
+    accepted: torch.Tensor      # [B] int32: accepted drafts
+    tokens: torch.Tensor        # [B, D + 1] int64: they, the drawn token, then -1
+    logp: torch.Tensor          # [B, D + 1] fp32: the policy's log-probs of the tokens, then 0
+
+
+def _rows3(t, name, B, rows, V, dtype, dev):
+    if t.dtype != dtype or tuple(t.shape) != (B, rows, V) or t.device != dev or \
+            (V > 1 and _plain(t, name).stride(2) != 1):
+        raise ValueError(f"{name} must be a [{B}, {rows}, {V}] {dtype} tensor on {dev} with unit last stride")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def verify_drafts(target_logits, draft_ids, accept_u, sample_u, draft_logits=None, num_drafts=None, *,
+                  temperature: float = 1.0) -> VerifyResult:
+    """Speculative decoding's check of drafted tokens: draft_ids [B, D] int64 against the policy's
+    target_logits [B, D + 1, V] (row i behind i drafts), with the draft model's draft_logits
+    [B, D, V] (None: drafts without a distribution) and the caller's uniform numbers accept_u
+    [B, D] and sample_u [B] in [0, 1). num_drafts [B] int32: a sequence's own number of drafts.
+    Returns the accepted count, the emitted tokens (accepted drafts and one drawn token) and their
+    log-probs under the policy, the logp_mu_old of the loss calls."""
+    if target_logits.dim() != 3 or not target_logits.is_cuda:
+        raise ValueError("target_logits must be a [B, D + 1, V] GPU tensor")
+    B, D1, V = target_logits.shape
+    D = D1 - 1
+    if D < 0:
+        raise ValueError("target_logits needs a row behind the last draft")
+    dev = target_logits.device
+    code = _dtype_code(target_logits)
+    t_ptr, t_seq, t_row = _rows3(target_logits, "target_logits", B, D1, V, target_logits.dtype, dev)
+    q_ptr, q_seq, q_row = (None, 0, 0) if draft_logits is None else \
+        _rows3(draft_logits, "draft_logits", B, D, V, target_logits.dtype, dev)
+    ids = _tensor(draft_ids, (B, D), torch.int64, "draft_ids", dev)
+    u = _tensor(accept_u, (B, D), torch.float32, "accept_u", dev)
+    un = _tensor(sample_u, (B,), torch.float32, "sample_u", dev)
+    num = None if num_drafts is None else _tensor(num_drafts, (B,), torch.int32, "num_drafts", dev)
+    n = _lib.lib().verify_drafts_workspace_bytes(code, B, D, V, int(draft_logits is not None and D > 0))
+    out = VerifyResult(accepted=torch.empty(B, dtype=torch.int32, device=dev),
+                       tokens=torch.empty(B, D1, dtype=torch.int64, device=dev),
+                       logp=torch.empty(B, D1, dtype=torch.float32, device=dev))
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n > 0 else None
+    with _on_device(dev):
+        st = _lib.lib().verify_drafts(
+            t_ptr, t_seq, t_row, q_ptr, q_seq, q_row, code, B, D, V, ids, num, u, un,
+            float(temperature), out.accepted.data_ptr(), out.tokens.data_ptr(), out.logp.data_ptr(),
+            ws.data_ptr() if ws is not None else None, max(n, 0), _stream(dev))
+    _lib.check(st, "verify_drafts")
+    return out

@@ -21,6 +21,7 @@ FLAG_VALID, FLAG_BAND, FLAG_PPO, FLAG_BAD_ID = 1, 2, 4, 8
 STAT_N_VALID, STAT_N_BAND, STAT_N_PPO, STAT_N_ACTIVE, STAT_N_BAD = range(5)
 N_STATS = 5
 MAX_VERSIONS = 8
+MAX_TOP = 256
 DTYPE_F32, DTYPE_BF16 = 0, 1
 ABI_VERSION = 6
 
@@ -84,6 +85,13 @@ SIGNATURES = {
                                                  VP, VP, C.POINTER(I64), VP]),
     "fused_lm_head_noalloc_scratch_bytes": (I64, []),
     "logprob_fwd_versioned": (I32, [C.POINTER(VP), I32, I32, I64, I64, I64, VP, VP, VP, VP, VP]),
+    "top_logits": (I32, [VP, I32, I64, I64, I64, I32, F64, VP, VP, VP, VP, I64, VP]),
+    "top_logits_workspace_bytes": (I64, [I32, I64, I64, I32]),
+    "distill_loss_fwd_bwd": (I32, [VP, I32, I64, I64, I64, VP, VP, I32, VP, VP, VP, F64, I32, F32,
+                                   VP, VP, VP, VP, VP, I64, VP]),
+    "verify_drafts": (I32, [VP, I64, I64, VP, I64, I64, I32, I64, I64, I64, VP, VP, VP, VP, F64,
+                            VP, VP, VP, VP, I64, VP]),
+    "verify_drafts_workspace_bytes": (I64, [I32, I64, I64, I64, I32]),
     "dppo_effective_thresholds": (I32, [C.c_double, C.c_double, C.c_double, C.c_double,
                                         C.c_double, I32, C.POINTER(C.c_double)]),
     "dppo_beta_from_window": (I32, [F64, C.POINTER(C.c_double)]),

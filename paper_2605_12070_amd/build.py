@@ -22,7 +22,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libdppo.so")
 SOURCES = ["loss_stage.hip", "lm_head.hip", "lm_head_grad.hip", "ewma.hip", "vocab_shard.hip", "grad_scale.hip",
-           "abi.hip"]
+           "distill.hip", "top_logits.hip", "verify.hip", "abi.hip"]
 ARCH = "gfx950"
 
 FLAGS = [

@@ -11,12 +11,15 @@
 #include <vector>
 
 #include "dppo.h"
+#include "distill.h"
 #include "dppo_device.h"
 #include "ewma.h"
 #include "grad_scale.h"
 #include "lm_head.h"
 #include "vocab_shard.h"
 #include "loss_stage.h"
+#include "top_logits.h"
+#include "verify.h"
 
 
 namespace {
@@ -1030,6 +1033,209 @@ dppo_status decoupled_ppo_loss_shard_fwd_bwd(
   e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "loss_sum launch");
   return DPPO_OK;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ teacher records and drafts
+namespace {
+
+// Matrix, temperature and record width of the calls below. Their kernels hold byte offsets within a
+// row in 32 bits.
+dppo_status check_rows(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
+                       double temperature, const char* name) {
+  const dppo_status s = check_matrix(logits, dtype, T, V, ld, name);
+  if (s != DPPO_OK) return s;
+  if (V > (int64_t)1 << 28) return fail(DPPO_ERR_INVALID_ARG, "V = %lld out of [1, 2^28]", (long long)V);
+  if ((uintptr_t)logits & (uintptr_t)(esize_of(dtype) - 1))
+    return fail(DPPO_ERR_INVALID_ARG, "%s must be aligned to its entries", name);
+  if (!(temperature > 0.0) || !std::isfinite((float)temperature) || !std::isfinite((float)(1.0 / temperature)))
+    return fail(DPPO_ERR_INVALID_ARG, "temperature = %g must be positive and finite, like its inverse",
+                temperature);
+  return DPPO_OK;
+}
+
+dppo_status check_workspace(const void* p, int64_t bytes, int64_t need) {
+  if (need > 0 && (!p || bytes < need))
+    return fail(DPPO_ERR_INVALID_ARG, "workspace of %lld bytes needed, %lld given", (long long)need,
+                (long long)bytes);
+  if (need > 0 && !aligned16(p)) return fail(DPPO_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  return DPPO_OK;
+}
+
+// Bytes of the parts' candidates, and with their sums of exponentials behind them.
+int64_t top_cand_bytes(int64_t T, int32_t k, int parts) { return (T * parts * k * 8 + 15) & ~(int64_t)15; }
+
+}  // namespace
+
+extern "C" {
+
+int64_t top_logits_workspace_bytes(int32_t dtype, int64_t T, int64_t V, int32_t k) {
+  if ((dtype != DPPO_F32 && dtype != DPPO_BF16) || T < 0 || T > 0x7FFFFFFF || V < 1 ||
+      V > (int64_t)1 << 28 || k < 1 || k > DPPO_MAX_TOP || k > V)
+    return -1;
+  const int parts = dppo::top_parts(T, V, esize_of(dtype));
+  return parts > 1 ? top_cand_bytes(T, k, parts) + T * parts * 8 : 0;
+}
+
+dppo_status top_logits(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld, int32_t k,
+                       double temperature, float* values_out, int32_t* ids_out, float* lse_out,
+                       void* workspace, int64_t workspace_bytes, void* stream) {
+  dppo_status s = check_rows(logits, dtype, T, V, ld, temperature, "logits");
+  if (s != DPPO_OK) return s;
+  if (k < 1 || k > DPPO_MAX_TOP || k > V)
+    return fail(DPPO_ERR_INVALID_ARG, "k = %d out of [1, min(V, %d)]", (int)k, DPPO_MAX_TOP);
+  if (T > 0 && (!values_out || !ids_out || !lse_out))
+    return fail(DPPO_ERR_INVALID_ARG, "values_out, ids_out and lse_out are required");
+  s = check_workspace(workspace, workspace_bytes, top_logits_workspace_bytes(dtype, T, V, k));
+  if (s != DPPO_OK) return s;
+  if (T == 0) return DPPO_OK;
+  dppo::TopArgs a{};
+  a.logits = logits;
+  a.ld = ld;
+  a.T = (int32_t)T;
+  a.V = (int32_t)V;
+  a.k = k;
+  a.parts = dppo::top_parts(T, V, esize_of(dtype));
+  a.l2e = (float)(1.44269504088896340736 / temperature);
+  a.values = values_out;
+  a.ids = ids_out;
+  a.lse = lse_out;
+  a.cand = (uint64_t*)workspace;
+  a.part = (float*)((char*)workspace + top_cand_bytes(T, k, a.parts));
+  const hipError_t e = dppo::launch_top_logits(a, dtype == DPPO_BF16, (hipStream_t)stream);
+  return e == hipSuccess ? DPPO_OK : hip_fail(e, "top logits launch");
+}
+
+dppo_status distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
+                                 const float* teacher_values, const int32_t* teacher_ids, int32_t k,
+                                 const float* teacher_lse, const uint8_t* loss_mask,
+                                 const float* token_scale, double temperature, int32_t scale_mode,
+                                 float loss_scale, float* kl_out, float* loss_out, uint8_t* flags_out,
+                                 int32_t* stats_out, void* dlogits, int64_t ld_dlogits, void* stream) {
+  dppo_status s = check_rows(logits, dtype, T, V, ld, temperature, "logits");
+  if (s != DPPO_OK) return s;
+  if (k < 1 || k > DPPO_MAX_TOP) return fail(DPPO_ERR_INVALID_ARG, "k = %d out of [1, %d]", (int)k, DPPO_MAX_TOP);
+  if (!loss_out || !stats_out) return fail(DPPO_ERR_INVALID_ARG, "loss_out and stats_out are required");
+  if (T > 0 && (!teacher_values || !teacher_ids || !kl_out || !flags_out))
+    return fail(DPPO_ERR_INVALID_ARG, "teacher_values, teacher_ids, kl_out and flags_out are required");
+  if (scale_mode != DPPO_SCALE_CONST && scale_mode != DPPO_SCALE_TOKEN_MEAN)
+    return fail(DPPO_ERR_INVALID_ARG, "unknown scale_mode %d", (int)scale_mode);
+  if (!std::isfinite(loss_scale)) return fail(DPPO_ERR_INVALID_ARG, "loss_scale must be finite");
+  const int es = esize_of(dtype);
+  if (dlogits && T > 0) {
+    if (ld_dlogits < V)
+      return fail(DPPO_ERR_INVALID_ARG, "dlogits stride %lld < V = %lld", (long long)ld_dlogits, (long long)V);
+    if ((uintptr_t)dlogits & (uintptr_t)(es - 1))
+      return fail(DPPO_ERR_INVALID_ARG, "dlogits must be aligned to its entries");
+    const bool same = dlogits == logits && ld_dlogits == ld;
+    if (!same && overlaps(span_of(logits, T, V, ld, es), span_of(dlogits, T, V, ld_dlogits, es)))
+      return fail(DPPO_ERR_INVALID_ARG, "dlogits overlaps logits without aliasing them exactly");
+  }
+  hipStream_t st = (hipStream_t)stream;
+  // a batch short enough for every workgroup to read its mask needs no counting kernel
+  const bool count_mode = T > 0 && T <= dppo::kCountModeMaxT;
+  hipError_t e = hipSuccess;
+  if (!count_mode) {
+    dppo::launch_prep_stats(loss_mask, T, stats_out, st);
+    e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, "prep_stats launch");
+  }
+  if (T > 0) {
+    dppo::DistillArgs a{};
+    a.logits = logits;
+    a.ld = ld;
+    a.dlogits = dlogits;
+    a.ldd = ld_dlogits;
+    a.mask = loss_mask;
+    a.tscale = token_scale;
+    a.loss_tok = kl_out;
+    a.flags = flags_out;
+    a.stats = stats_out;
+    a.T = (int32_t)T;
+    a.V = (int32_t)V;
+    a.mode = dppo::kModeLoss;
+    a.loss_scale = loss_scale;
+    a.scale_mode = scale_mode;
+    a.count_mode = count_mode ? 1 : 0;
+    a.values = teacher_values;
+    a.tokens = teacher_ids;
+    a.tlse = teacher_lse;
+    a.k = k;
+    a.t2e = 1.44269504088896340736 / temperature;
+    a.l2e = (float)a.t2e;
+    a.inv_tau = 1.0 / temperature;
+    e = dppo::launch_distill(a, dtype == DPPO_BF16, st);
+    if (e != hipSuccess) return hip_fail(e, "distillation launch");
+  }
+  dppo::launch_loss_sum(kl_out, loss_mask, token_scale, stats_out, T, loss_scale, scale_mode, loss_out,
+                        st, T > 0 ? flags_out : nullptr, DPPO_RD_NONE);
+  e = hipGetLastError();
+  return e == hipSuccess ? DPPO_OK : hip_fail(e, "loss_sum launch");
+}
+
+namespace {
+constexpr int64_t kMaxDrafts = 1024;
+}
+
+int64_t verify_drafts_workspace_bytes(int32_t dtype, int64_t B, int64_t D, int64_t V, int32_t with_draft) {
+  if ((dtype != DPPO_F32 && dtype != DPPO_BF16) || B < 0 || B > 1 << 20 || D < 0 || D > kMaxDrafts ||
+      V < 1 || V > (int64_t)1 << 28)
+    return -1;
+  dppo::VerifyArgs a{};
+  a.B = (int32_t)B;
+  a.D = (int32_t)D;
+  a.V = (int32_t)V;
+  return dppo::verify_layout(a, esize_of(dtype), with_draft != 0, nullptr);
+}
+
+dppo_status verify_drafts(const void* target, int64_t target_seq, int64_t target_row, const void* draft,
+                          int64_t draft_seq, int64_t draft_row, int32_t dtype, int64_t B, int64_t D,
+                          int64_t V, const int64_t* draft_ids, const int32_t* num_drafts,
+                          const float* accept_u, const float* sample_u, double temperature,
+                          int32_t* accepted_out, int64_t* tokens_out, float* logp_out, void* workspace,
+                          int64_t workspace_bytes, void* stream) {
+  if (B < 0 || B > 1 << 20) return fail(DPPO_ERR_INVALID_ARG, "B = %lld out of [0, 2^20]", (long long)B);
+  if (D < 0 || D > kMaxDrafts)
+    return fail(DPPO_ERR_INVALID_ARG, "D = %lld out of [0, %lld]", (long long)D, (long long)kMaxDrafts);
+  // strides that no second row or sequence uses may be anything
+  const int64_t tr = D > 0 ? target_row : V, ts = B > 1 ? target_seq : V;
+  dppo_status s = check_rows(target, dtype, B, V, std::min(tr, ts), temperature, "target");
+  if (s != DPPO_OK) return s;
+  if (draft && D > 0) {
+    const int64_t dr = D > 1 ? draft_row : V, ds = B > 1 ? draft_seq : V;
+    s = check_rows(draft, dtype, B, V, std::min(dr, ds), temperature, "draft");
+    if (s != DPPO_OK) return s;
+  }
+  if (B > 0 && (!sample_u || !accepted_out || !tokens_out || !logp_out))
+    return fail(DPPO_ERR_INVALID_ARG, "sample_u, accepted_out, tokens_out and logp_out are required");
+  if (B > 0 && D > 0 && (!draft_ids || !accept_u))
+    return fail(DPPO_ERR_INVALID_ARG, "draft_ids and accept_u are required");
+  const bool with_draft = draft != nullptr && D > 0;
+  s = check_workspace(workspace, workspace_bytes, B > 0 ? verify_drafts_workspace_bytes(dtype, B, D, V, with_draft) : 0);
+  if (s != DPPO_OK) return s;
+  if (B == 0) return DPPO_OK;
+  dppo::VerifyArgs a{};
+  a.target = target;
+  a.target_seq = target_seq;
+  a.target_row = target_row;
+  a.draft = with_draft ? draft : nullptr;
+  a.draft_seq = draft_seq;
+  a.draft_row = draft_row;
+  a.B = (int32_t)B;
+  a.D = (int32_t)D;
+  a.V = (int32_t)V;
+  a.ids = draft_ids;
+  a.num = num_drafts;
+  a.u = accept_u;
+  a.u_new = sample_u;
+  a.t2e = 1.44269504088896340736 / temperature;
+  a.accepted = accepted_out;
+  a.tokens = tokens_out;
+  a.logp = logp_out;
+  dppo::verify_layout(a, esize_of(dtype), with_draft, workspace);
+  const hipError_t e = dppo::launch_verify(a, dtype == DPPO_BF16, (hipStream_t)stream);
+  return e == hipSuccess ? DPPO_OK : hip_fail(e, "draft verification launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,22 @@
+// Internal interface of the distillation kernels.
+#pragma once
+
+#include "loss_stage.h"
+
+namespace dppo {
+
+// The row arguments (logits, dlogits, mask, token scale, flags, stats, scale; loss_tok is the
+// per-token loss) and the teacher's record.
+struct DistillArgs : RowArgs {
+  const float* values;    // [T, k]
+  const int32_t* tokens;  // [T, k], -1: empty
+  const float* tlse;      // [T] the teacher's log-sum-exp, NULL: the record is renormalised
+  int32_t k;
+  float l2e;              // log2(e) / temperature, as the kernels use it on the student's logits
+  double t2e;             // the same in 64 bits, for the record's values
+  double inv_tau;
+};
+
+hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st);
+
+}  // namespace dppo

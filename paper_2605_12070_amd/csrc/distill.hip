@@ -1,0 +1,431 @@
+// Distillation from a teacher's top logits: per row the divergence between the teacher's record (k
+// values with their token ids) and the student's softmax, and its gradient, with the logits read
+// once and dlogits written once.
+//
+// With q = softmax(z / tau), p the record's probabilities, P = sum p, Q = sum of q over the record's
+// tokens:
+//   renormalised record: l = sum p_k (log p_k - log q_k),              f = g = P
+//   with the tail:       l + Pt log(Pt / Qt), Pt = 1 - P, Qt = 1 - Q,  f = P - Pt Q / Qt, g = P + Pt
+//   dz_v = s / tau * f q_v outside the record, s / tau * (g q_v - p_v) inside it.
+// Qt is summed over the entries outside the record: 1 - Q would lose it where the student is nearly
+// sure of the record's tokens. So the record's entries leave the sum of exponentials when their
+// chunk is read, and the record's own exponentials join it afterwards.
+//
+// A workgroup handles a row (persistent, looping over rows). The row's first NT NC 16-byte chunks
+// stay in registers as they were read, the next KS NT in LDS, and only the rest of a longer row is
+// read again for the gradient. Every entry belongs to one thread (RowSplit; chunk c to thread
+// c mod NT), which finds the record's tokens among its entries in a list of its own (built in LDS by
+// the threads that hold the record); a bit per chunk slot tells it which chunks to look at. The
+// record's own arithmetic runs in 64 bits on one wave: k is small, and the loss is a difference of
+// log-probabilities.
+#include "distill.h"
+
+#include <algorithm>
+
+#include "dppo_device.h"
+#include "f64_math.h"
+#include "row_common.h"
+#include "row_split.h"
+
+namespace dppo {
+
+namespace {
+
+constexpr int kMaxK = DPPO_MAX_TOP;
+// Least tail mass a student is given: the tail's gradient carries 1 / Qt.
+constexpr double kTailFloor = 5.9604644775390625e-08;   // 2^-24
+
+// A row's record in LDS. Two of them alternate between the rows that are evaluated: threads still
+// in one row's gradient read its record while others prepare the next row's.
+template <int NT>
+struct Record {
+  int head[NT];        // first record entry in a thread's list, -1: none; reset by its thread
+  int16_t next[kMaxK];
+  int id[kMaxK];
+  float grad[kMaxK];   // dlogits at the entry's token
+  uint8_t again[kMaxK];  // the token stands at a lower place of the record too
+};
+
+struct RecordMath {    // one row at a time, between two barriers
+  float value[kMaxK];
+  float z[kMaxK];
+  double p[kMaxK], q[kMaxK];
+  int any_again;
+  float w, lse2;
+};
+
+__device__ __forceinline__ double wave_sum_f64(double v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+__device__ __forceinline__ double wave_max_f64(double v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v = fmax(v, __shfl_xor(v, off, 64));
+  return v;
+}
+
+// The record's part of a row, by one wave: lane holds entries lane, lane + 64, ... N, S: the sum of
+// exponentials outside the record (2^N S, in log2 units). Everything an entry needs waits in LDS and
+// the loops are not unrolled: next to a row in registers there is no room for more.
+template <class Rec>
+__device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, float scale, float N, float S,
+                                            Rec& rec, RecordMath& m) {
+  const int lane = threadIdx.x & 63;
+  const int k = a.k;
+  const double zl = (double)a.l2e;
+  // -inf marks an empty entry here: its probability and its term are 0 either way
+  double tm = -INFINITY, zm = N;
+#pragma unroll 1
+  for (int j = lane; j < k; j += 64) {
+    tm = fmax(tm, (double)m.value[j] * a.t2e);
+    zm = fmax(zm, (double)m.z[j] * zl);
+  }
+  zm = wave_max_f64(zm);
+  tm = wave_max_f64(tm);
+  const double zs = zm == -INFINITY ? 0.0 : zm;
+  // the sums of exponentials around the maxima
+  double st = 0.0, sq = 0.0;
+#pragma unroll 1
+  for (int j = lane; j < k; j += 64) {
+    const double tj = (double)m.value[j] * a.t2e;
+    if (tj != -INFINITY) st += exp2_f64(tj - tm);
+    if (!rec.again[j]) sq += exp2_f64((double)m.z[j] * zl - zs);
+  }
+  sq = wave_sum_f64(sq);
+  double c;
+  if (a.tlse) {
+    c = (double)a.tlse[row] * kLog2eF64;
+  } else {
+    st = wave_sum_f64(st);
+    c = st == 0.0 ? 0.0 : tm + log2_f64(st);   // 0: an empty record, or one of -inf alone
+  }
+  const double rest = N == -INFINITY ? 0.0 : (double)S * exp2_f64((double)N - zs);
+  const double total = sq + rest;
+  const double lse2 = zm == -INFINITY ? (double)__builtin_nanf("") : zs + log2_f64(total);
+  double l = 0.0, P = 0.0, Q = 0.0;
+#pragma unroll 1
+  for (int j = lane; j < k; j += 64) {
+    const double tj = (double)m.value[j] * a.t2e;
+    const double lq = (double)m.z[j] * zl - lse2;
+    const double p = tj == -INFINITY ? 0.0 : exp2_f64(tj - c);
+    const double q = rec.id[j] < 0 ? 0.0 : exp2_f64(lq);
+    if (p != 0.0) l += p * ((tj - c) - lq) * kLn2F64;
+    P += p;
+    if (!rec.again[j]) Q += q;
+    m.p[j] = p;
+    m.q[j] = q;
+  }
+  l = wave_sum_f64(l);
+  P = wave_sum_f64(P);
+  double f = P, g = P;
+  if (a.tlse) {
+    Q = wave_sum_f64(Q);
+    const double Pt = 1.0 - P > 0.0 ? 1.0 - P : 0.0;
+    const double Qt = fmax(rest / total, kTailFloor);
+    if (Pt > 0.0) l += Pt * log2_f64(Pt / Qt) * kLn2F64;
+    f = P - Pt * Q / Qt;
+    g = P + Pt;
+  }
+  const double s = (double)scale * a.inv_tau;
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+#pragma unroll 1
+  for (int j = lane; j < k; j += 64) {
+    double p = m.p[j];
+    if (m.any_again)
+      for (int i = j + 1; i < k; ++i)
+        if (rec.id[i] == rec.id[j]) p += m.p[i];
+    rec.grad[j] = (float)(s * (g * m.q[j] - p));
+  }
+  if (lane == 0) {
+    // what rounding lse2 to 32 bits leaves over goes into the factor
+    const float l2 = (float)lse2;
+    m.lse2 = l2;
+    m.w = (float)(s * f * exp2_f64((double)l2 - lse2));
+    a.loss_tok[row] = (float)l;
+  }
+}
+
+template <typename Tin, int NT, int NC, int KS>
+__global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
+  constexpr int E = 16 / (int)sizeof(Tin);
+  constexpr int P = NT * NC;               // chunks of a row in registers
+  constexpr int U = 4;                     // further chunks per thread in flight
+  constexpr int kOff = 0x7fffff00;
+  __shared__ float red[2][2 * (NT / 64)];
+  __shared__ Record<NT> recs[2];
+  __shared__ RecordMath rm;
+  __shared__ u32x4 keep[KS > 0 ? KS * NT : 1];
+  const int tid = threadIdx.x;
+  const int V = a.V;
+  const float L = a.l2e;
+  recs[0].head[tid] = recs[1].head[tid] = -1;
+  const float scale = call_scale<NT>(a);
+  auto is_valid = [&](int64_t row) { return a.mask == nullptr || uload_u8(a.mask + row) != 0; };
+  uint32_t r[NC][4];
+  auto load_row = [&](int64_t row, bool rd) {
+    const Tin* z = (const Tin*)a.logits + (rd ? row : 0) * a.ld;
+    const RowSplit sp = split_row(z, V);
+    const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + sp.lead, rd ? sp.nfull * 16 : 0);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) load16<kAuxLast>(r[c], rz, tid * 16, c * NT * 16);
+  };
+  auto unpack = [&](const auto& v, float (&x)[E]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (sizeof(Tin) == 2) {
+        x[2 * j] = bf16_lo(v[j]);
+        x[2 * j + 1] = bf16_hi(v[j]);
+      } else {
+        x[j] = __uint_as_float(v[j]);
+      }
+    }
+  };
+  int64_t row = blockIdx.x;
+  bool valid = row < a.T && is_valid(row);
+  load_row(row, valid);
+  __syncthreads();                         // the lists are empty
+  int parity = 0;                          // flips after each row that was evaluated
+  for (; row < a.T; row += gridDim.x) {
+    const int64_t next = row + gridDim.x;
+    const bool next_valid = next < a.T && is_valid(next);
+    Tin* drow = a.dlogits ? (Tin*)a.dlogits + row * a.ldd : nullptr;
+    if (!valid) {
+      if (drow) zero_row<Tin, NT>(drow, V);
+      if (tid == 0) {
+        a.loss_tok[row] = 0.0f;
+        a.flags[row] = 0;
+      }
+      load_row(next, next_valid);
+      valid = next_valid;
+      continue;
+    }
+    Record<NT>& rec = recs[parity];
+    const Tin* zrow = (const Tin*)a.logits + row * a.ld;
+    const RowSplit sp = split_row(zrow, V);
+    const int nfull = sp.nfull;
+    const bool edge = tid < sp.nedge;
+    const int ei = sp.template entry<E>(tid);
+    // the record: thread j holds entry j and hands it to the thread that owns its token
+    int id = -1;
+    float tv = 0.0f, tz = 0.0f;
+    bool bad = false;
+    if (tid < a.k) {
+      id = a.tokens[row * a.k + tid];
+      tv = a.values[row * a.k + tid];
+      bad = id < -1 || id >= V;
+      id = bad ? -1 : id;
+      rec.id[tid] = id;
+      rec.again[tid] = 0;
+      if (id >= 0) {
+        tz = sizeof(Tin) == 2 ? bf16_to_f32(((const uint16_t*)zrow)[id]) : ((const float*)zrow)[id];
+        const int e = id - sp.lead;
+        const int owner = e >= 0 && e < nfull * E ? (e / E) % NT : (e < 0 ? id : id - nfull * E);
+        rec.next[tid] = (int16_t)atomicExch(&rec.head[owner], tid);
+      }
+    }
+    if (tid == 0) rm.any_again = 0;
+    if (__syncthreads_or(bad)) {           // a token outside the vocabulary: the row counts as bad
+      rec.head[tid] = -1;
+      parity ^= 1;
+      if (drow) zero_row<Tin, NT>(drow, V);
+      if (tid == 0) {
+        a.loss_tok[row] = 0.0f;
+        a.flags[row] = (uint8_t)(DPPO_FLAG_VALID | DPPO_FLAG_BAD_ID);
+      }
+      load_row(next, next_valid);
+      valid = next_valid;
+      continue;
+    }
+    const int head = rec.head[tid];
+    uint32_t slots = 0;                    // bit s mod 32: a record's token lies in chunk slot s
+    bool edge_held = false;
+    for (int j = head; j >= 0; j = rec.next[j]) {
+      const int e = rec.id[j] - sp.lead;
+      if (e >= 0 && e < nfull * E) slots |= 1u << ((e / E / NT) & 31);
+      else edge_held = true;
+      for (int j2 = rec.next[j]; j2 >= 0; j2 = rec.next[j2])
+        if (rec.id[j2] == rec.id[j]) {
+          rec.again[j > j2 ? j : j2] = 1;
+          rm.any_again = 1;
+        }
+    }
+    // the record's entries of chunk idx (this thread's): f(j, entry of the chunk)
+    auto held = [&](int idx, auto&& f) {
+      for (int j = head; j >= 0; j = rec.next[j]) {
+        const int e = rec.id[j] - sp.lead - idx * E;
+        if (e >= 0 && e < E) f(j, e);
+      }
+    };
+    float N = -INFINITY, S = 0.0f;
+    auto add = [&](float (&x)[E], int slot) {
+      if (slots >> (slot & 31) & 1u)
+        held(slot * NT + tid, [&](int, int e) {
+#pragma unroll
+          for (int i = 0; i < E; ++i) x[i] = i == e ? -INFINITY : x[i];
+        });
+      float cm = max3(x[0], x[1], x[2]);
+      if constexpr (E == 8) cm = max3(cm, max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
+      else cm = fmaxf(cm, x[3]);
+      const float nc = __builtin_ceilf(cm * L);
+      const float sh = (nc == -INFINITY) ? 0.0f : nc;
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) s += exp2_hw(__builtin_fmaf(x[i], L, -sh));
+      merge_ns_int(N, S, nc, s);
+    };
+    const __amdgpu_buffer_rsrc_t rz = row_rsrc(zrow + sp.lead, nfull * 16);
+    // chunks past the registers first, so that their registers and the row's are not live together
+    if constexpr (KS > 0) {
+      for (int i0 = P + tid, s0 = NC; i0 < nfull; i0 += U * NT, s0 += U) {
+        u32x4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int idx = i0 + u * NT;
+          v[u] = buf_load16(rz, idx < nfull ? idx * 16 : kOff, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (s0 + u - NC < KS) keep[(s0 + u - NC) * NT + tid] = v[u];
+          if (i0 + u * NT >= nfull) continue;
+          float x[E];
+          unpack(v[u], x);
+          add(x, s0 + u);
+        }
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if (c * NT < nfull) {                // uniform
+        float x[E];
+        unpack(r[c], x);
+        if (c * NT + tid < nfull) add(x, c);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    float xe = -INFINITY;
+    if (edge) {
+      xe = sizeof(Tin) == 2 ? bf16_to_f32(((const uint16_t*)zrow)[ei]) : ((const float*)zrow)[ei];
+      bool own = false;
+      if (edge_held)
+        for (int j = head; j >= 0; j = rec.next[j]) own |= rec.id[j] == ei;
+      const float x = own ? -INFINITY : xe;
+      const float nc = __builtin_ceilf(x * L);
+      merge_ns_int(N, S, nc, nc == -INFINITY ? 0.0f : exp2_hw(__builtin_fmaf(x, L, -nc)));
+    }
+    if (tid < a.k) {
+      rm.value[tid] = id >= 0 ? tv : -INFINITY;
+      rm.z[tid] = id >= 0 ? tz : -INFINITY;
+    }
+    block_merge_ns_int<NT>(N, S, red[parity]);
+    if (tid < 64) record_math(a, row, scale * (a.tscale ? uload(a.tscale + row) : 1.0f), N, S, rec, rm);
+    if (tid == 0) a.flags[row] = (uint8_t)DPPO_FLAG_VALID;
+    parity ^= 1;
+    rec.head[tid] = -1;                    // this thread's list stays reachable through `head`
+    if (drow) {
+      __syncthreads();
+      const float w = rm.w, l2 = rm.lse2;
+      const __amdgpu_buffer_rsrc_t rd = row_rsrc(drow + sp.lead, nfull * 16);
+      const bool same = (((uintptr_t)drow - (uintptr_t)zrow) & 15) == 0;    // uniform
+      auto put = [&](const float (&x)[E], int slot) {
+        const int idx = slot * NT + tid;
+        float o[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) o[i] = w * exp2_hw(__builtin_fmaf(x[i], L, -l2));
+        if (slots >> (slot & 31) & 1u)
+          held(idx, [&](int j, int e) {
+            if (rec.again[j]) return;
+            const float gj = rec.grad[j];
+#pragma unroll
+            for (int i = 0; i < E; ++i) o[i] = i == e ? gj : o[i];
+          });
+        u32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (sizeof(Tin) == 2) v[i] = pack_bf16(o[2 * i], o[2 * i + 1]);
+          else v[i] = __float_as_uint(o[i]);
+        }
+        if (same) {
+          buf_store16_nt(v, rd, idx < nfull ? idx * 16 : kOff, 0);
+        } else if (idx < nfull) {
+          Tin* d = drow + sp.lead + idx * E;
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            if constexpr (sizeof(Tin) == 2) d[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+            else d[i] = o[i];
+          }
+        }
+      };
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        if (c * NT < nfull) {
+          float x[E];
+          unpack(r[c], x);
+          put(x, c);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (KS > 0) {
+        for (int i0 = P + tid, s0 = NC; i0 < nfull; i0 += U * NT, s0 += U) {
+          u32x4 v[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int idx = i0 + u * NT;
+            if (s0 + u - NC < KS) v[u] = keep[(s0 + u - NC) * NT + tid];
+            else v[u] = buf_load16<kAuxLast>(rz, idx < nfull ? idx * 16 : kOff, 0);
+          }
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (i0 + u * NT >= nfull) continue;
+            float x[E];
+            unpack(v[u], x);
+            put(x, s0 + u);
+          }
+        }
+      }
+      if (edge) {
+        float o = w * exp2_hw(__builtin_fmaf(xe, L, -l2));
+        if (edge_held)
+          for (int j = head; j >= 0; j = rec.next[j])
+            if (rec.id[j] == ei && !rec.again[j]) o = rec.grad[j];
+        if constexpr (sizeof(Tin) == 2) drow[ei] = to_bf16(o);
+        else drow[ei] = o;
+      }
+    }
+    load_row(next, next_valid);
+    valid = next_valid;
+  }
+}
+
+struct Shape {
+  int nt, nc;
+  const void *bf16, *f32;
+};
+template <int NT, int NC, int KS>
+constexpr Shape shape() {
+  return {NT, NC, (const void*)distill_rows<uint16_t, NT, NC, KS>, (const void*)distill_rows<float, NT, NC, KS>};
+}
+
+}  // namespace
+
+hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
+  // by the chunks of a row; the last takes rows of any length
+  static const Shape shapes[] = {shape<256, 2, 0>(), shape<256, 4, 0>(),   shape<256, 8, 0>(),   shape<512, 8, 0>(),
+                                 shape<1024, 8, 0>(), shape<1024, 12, 0>(), shape<1024, 19, 0>(), shape<1024, 16, 7>()};
+  const int64_t chunks = (int64_t)a.V * (bf16 ? 2 : 4) / 16;
+  const Shape* s = shapes;
+  while (s + 1 < shapes + sizeof(shapes) / sizeof(shapes[0]) && (int64_t)s->nt * s->nc < chunks) ++s;
+  const void* fn = bf16 ? s->bf16 : s->f32;
+  int dev = 0, cus = 0, per_cu = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, fn, s->nt, 0);
+  if (e != hipSuccess) return e;
+  const int64_t grid = std::min<int64_t>(a.T, (int64_t)cus * std::max(per_cu, 1));
+  DistillArgs args = a;
+  void* kargs[] = {&args};
+  e = hipLaunchKernel(fn, dim3((unsigned)grid), dim3((unsigned)s->nt), kargs, 0, st);
+  return e == hipSuccess ? hipGetLastError() : e;
+}
+
+}  // namespace dppo

@@ -1,0 +1,365 @@
+// The k largest logits of every row, best first (equal values by index), with the row's
+// log-sum-exp: one read of the logits.
+//
+// A bound that at least k entries reach lets almost every entry be dropped with one comparison. The
+// k-th largest of the threads' running maxima is such a bound: k different entries reach it. A
+// workgroup streams a row in tiles of U 16-byte chunks per thread; after the first tile, and each
+// time the part read has doubled, it takes that bound from the maxima so far, and entries that reach
+// the bound of their time are kept in LDS (k ln(tiles) of them in random order). At the end the kept
+// ones are ranked by counting, which needs no barrier. What the fast path cannot hold (long runs of
+// equal values, a row with NaN or infinities, fewer than k finite entries) is selected exactly by
+// radix passes over the row.
+#include "top_logits.h"
+
+#include <algorithm>
+
+#include "dppo_device.h"
+#include "row_split.h"
+
+namespace dppo {
+
+namespace {
+
+constexpr int kTopU = 8;         // 16-byte chunks per thread in flight
+// Kept entries. A row whose maxima are too few for a bound is kept whole: fewer than 256 chunks of 8
+// entries and two ends.
+constexpr int kTopCap = 2112;
+constexpr int kTopRank = 512;    // more than these are thinned out before the ranking
+
+// Unsigned keys in the order of the values: -0 as +0, NaN above +inf.
+__device__ __forceinline__ uint32_t value_key(float x) {
+  const uint32_t b = __float_as_uint(x + 0.0f);
+  if (x != x) return 0xFFFFFFFFu;
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+  if (k == 0xFFFFFFFFu) return __builtin_nanf("");
+  return __uint_as_float((k & 0x80000000u) ? (k ^ 0x80000000u) : ~k);
+}
+constexpr uint32_t kKeyLowest = 0x00800000u;  // the key of -FLT_MAX
+
+// Larger value first, then the lower index.
+__device__ __forceinline__ uint64_t composite(float x, int idx) {
+  return ((uint64_t)value_key(x) << 32) | (uint32_t)~idx;
+}
+
+template <typename Tin>
+__device__ __forceinline__ float entry_value(const Tin* p, int64_t i) {
+  if constexpr (sizeof(Tin) == 2) return bf16_to_f32(p[i]);
+  else return p[i];
+}
+
+template <typename Tin>
+__device__ __forceinline__ void unpack(const uint32_t (&r)[4], float (&x)[16 / sizeof(Tin)]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (sizeof(Tin) == 2) {
+      x[2 * k] = bf16_lo(r[k]);
+      x[2 * k + 1] = bf16_hi(r[k]);
+    } else {
+      x[k] = __uint_as_float(r[k]);
+    }
+  }
+}
+
+template <int E>
+__device__ __forceinline__ float max_of(const float (&x)[E]) {
+  if constexpr (E == 8) return max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
+  else return max3(max3(x[0], x[1], x[2]), x[3], x[3]);
+}
+
+// Output slot `rank` of a row (or of a row's part).
+__device__ __forceinline__ void put(const TopArgs& a, int64_t row, int part, int rank, uint64_t c) {
+  if (a.parts > 1) {
+    a.cand[(row * a.parts + part) * a.k + rank] = c;
+  } else {
+    a.values[row * a.k + rank] = key_value((uint32_t)(c >> 32));
+    a.ids[row * a.k + rank] = (int32_t)~(uint32_t)c;
+  }
+}
+
+template <typename Tin, int NT>
+__global__ __launch_bounds__(NT) void top_rows(TopArgs a) {
+  constexpr int E = 16 / (int)sizeof(Tin);
+  constexpr int U = kTopU;
+  constexpr int NW = NT / 64;
+  __shared__ uint64_t cand[kTopCap];
+  __shared__ uint64_t kept[kTopCap];
+  __shared__ uint32_t tkey[NT];
+  __shared__ float red[2 * NW];
+  __shared__ int wcount[NW];
+  __shared__ int hist[256];
+  __shared__ int count, kcount;
+  __shared__ uint32_t bound_s;
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int k = a.k;
+  const float L = a.l2e;
+  for (int64_t item = blockIdx.x; item < (int64_t)a.T * a.parts; item += gridDim.x) {
+    const int64_t row = item / a.parts;
+    const int part = (int)(item - row * a.parts);
+    const Tin* z = (const Tin*)a.logits + row * a.ld;
+    const RowSplit sp = split_row(z, a.V);
+    // this part's chunks [c0, c0 + n), and the row's single entries at its ends
+    const int c0 = (int)((int64_t)sp.nfull * part / a.parts);
+    const int n = (int)((int64_t)sp.nfull * (part + 1) / a.parts) - c0;
+    const int first = sp.lead + c0 * E;
+    const int le = part == 0 ? sp.lead : 0;
+    const int te = part == a.parts - 1 ? sp.nedge - sp.lead : 0;
+    const int e0 = part == 0 ? 0 : first;                      // the part's entries [e0, e1)
+    const int e1 = part == a.parts - 1 ? a.V : first + n * E;
+    const bool edge = tid < le + te;
+    const int ei = tid < le ? tid : sp.lead + sp.nfull * E + (tid - le);
+    const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + first, n * 16);
+    __syncthreads();                       // the last item's LDS is free
+    if (tid == 0) count = kcount = 0;
+
+    uint32_t r[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load16<kAuxLast>(r[u], rz, tid * 16, u * NT * 16);
+    float N = -INFINITY, S = 0.0f, tmax = -INFINITY;
+    auto add = [&](const auto& x, float cm) {
+      const float nc = __builtin_ceilf(cm * L);
+      const float sh = (nc == -INFINITY) ? 0.0f : nc;
+      float s = 0.0f;
+#pragma unroll
+      for (int j = 0; j < (int)(sizeof(x) / 4); ++j) s += exp2_hw(__builtin_fmaf(x[j], L, -sh));
+      merge_ns_int(N, S, nc, s);
+      tmax = fmaxf(tmax, cm);
+    };
+    float xe = -INFINITY;
+    if (edge) {
+      xe = entry_value(z, ei);
+      const float x[1] = {xe};
+      add(x, xe);
+    }
+    // the bound: the largest 16-bit key prefix that k threads' maxima reach
+    auto update_bound = [&]() -> float {
+      tkey[tid] = value_key(tmax);
+      __syncthreads();
+      if (wave == 0) {
+        uint32_t key[NW];
+#pragma unroll
+        for (int j = 0; j < NW; ++j) key[j] = tkey[j * 64 + lane];
+        uint32_t b = 0;
+        for (int bit = 31; bit >= 16; --bit) {
+          const uint32_t t = b | (1u << bit);
+          int c = 0;
+#pragma unroll
+          for (int j = 0; j < NW; ++j) c += __popcll(__ballot(key[j] >= t));
+          if (c >= k) b = t;
+        }
+        if (lane == 0) bound_s = b > kKeyLowest ? b : kKeyLowest;
+      }
+      __syncthreads();
+      return key_value(bound_s);
+    };
+    auto push = [&](float x, int idx) {
+      const int slot = atomicAdd(&count, 1);
+      if (slot < kTopCap) cand[slot] = composite(x, idx);
+    };
+    float bound = 0.0f;
+    auto test = [&](const float (&x)[E], float cm, int c) {
+      if (cm >= bound) {
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+          if (x[j] >= bound) push(x[j], first + c * E + j);
+      }
+    };
+    // first tile: the maxima, their bound, then the entries that reach it
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u * NT >= n) break;              // uniform
+      float x[E];
+      unpack<Tin>(r[u], x);
+      if (u * NT + tid < n) add(x, max_of(x));
+    }
+    bound = update_bound();
+    if (edge && xe >= bound) push(xe, ei);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u * NT >= n) break;
+      float x[E];
+      unpack<Tin>(r[u], x);
+      if ((U + u) * NT < n) load16<kAuxLast>(r[u], rz, tid * 16, (U + u) * NT * 16);
+      if (u * NT + tid < n) test(x, max_of(x), u * NT + tid);
+    }
+    int t = 1;
+    for (int b = U * NT; b < n; b += U * NT, ++t) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (b + u * NT >= n) break;
+        float x[E];
+        unpack<Tin>(r[u], x);
+        if (b + (U + u) * NT < n) load16<kAuxLast>(r[u], rz, tid * 16, (b + (U + u) * NT) * 16);
+        if (b + u * NT + tid < n) {
+          const float cm = max_of(x);
+          add(x, cm);
+          test(x, cm, b + u * NT + tid);
+        }
+      }
+      if ((t & (t + 1)) == 0 && b + U * NT < n) bound = update_bound();
+    }
+    block_merge_ns_int<NT>(N, S, red);     // its barrier also makes `count` final
+    int m = count;
+    const uint64_t* list = cand;
+    const int kk = k < e1 - e0 ? k : e1 - e0;
+    if (m > kTopCap || m < kk || !(S < INFINITY)) {
+      // exact: the key of the kk-th entry by radix passes, then everything above it and the first
+      // of its equals
+      __syncthreads();
+      uint32_t prefix = 0, mask = 0;
+      int need = kk;
+      for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = tid; i < 256; i += NT) hist[i] = 0;
+        __syncthreads();
+        for (int e = e0 + tid; e < e1; e += NT) {
+          const uint32_t key = value_key(entry_value(z, e));
+          if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1);
+        }
+        __syncthreads();
+        int bin = 255;
+        for (int above = hist[bin]; above < need; above = hist[bin]) {
+          need -= above;
+          --bin;
+        }
+        prefix |= (uint32_t)bin << shift;
+        mask |= 255u << shift;
+        __syncthreads();
+      }
+      if (tid == 0) count = 0;
+      int before = 0;                      // equals before this step
+      __syncthreads();
+      for (int base = e0; base < e1; base += NT) {
+        const int e = base + tid;
+        const float x = e < e1 ? entry_value(z, e) : 0.0f;
+        const uint32_t key = value_key(x);
+        if (e < e1 && key > prefix) push(x, e);
+        const bool tie = e < e1 && key == prefix;
+        const uint64_t ties = __ballot(tie);
+        if (lane == 0) wcount[wave] = __popcll(ties);
+        __syncthreads();
+        int at = before + __popcll(ties & ((1ull << lane) - 1ull));
+        for (int w = 0; w < NW; ++w) {
+          if (w < wave) at += wcount[w];
+          before += wcount[w];
+        }
+        if (tie && at < need) push(x, e);
+        __syncthreads();
+      }
+      m = kk;
+    } else if (m > kTopRank) {
+      // thin out: a key that at least k and, if the keys allow it, at most kTopRank entries reach
+      uint32_t b = 0;
+      int reach = m;
+      for (int bit = 31; bit >= 0 && reach > kTopRank; --bit) {
+        const uint32_t key = b | (1u << bit);
+        int c = 0;
+        for (int i = tid; i < m; i += NT) c += (uint32_t)(cand[i] >> 32) >= key;
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off, 64);
+        if (lane == 0) wcount[wave] = c;
+        __syncthreads();
+        c = 0;
+        for (int w = 0; w < NW; ++w) c += wcount[w];
+        __syncthreads();
+        if (c >= k) {
+          b = key;
+          reach = c;
+        }
+      }
+      for (int i = tid; i < m; i += NT) {
+        const uint64_t c = cand[i];
+        if ((uint32_t)(c >> 32) >= b) kept[atomicAdd(&kcount, 1)] = c;
+      }
+      __syncthreads();
+      list = kept;
+      m = kcount;
+    }
+    for (int i = tid; i < m; i += NT) {
+      const uint64_t c = list[i];
+      int rank = 0;
+      for (int j = 0; j < m; ++j) rank += list[j] > c;
+      if (rank < k) put(a, row, part, rank, c);
+    }
+    for (int i = kk + tid; i < k; i += NT) put(a, row, part, i, 0);   // a part shorter than k
+    if (tid == 0) {
+      if (a.parts > 1) {
+        a.part[2 * item] = N;
+        a.part[2 * item + 1] = S;
+      } else {
+        a.lse[row] = (N == -INFINITY) ? __builtin_nanf("") : (N + log2f(S)) * kLn2;
+      }
+    }
+  }
+}
+
+// Joins a row's parts: an entry's rank is its place in its own part's list and the number of larger
+// ones in each other list (a binary search: the lists are sorted).
+constexpr int kJoinNT = 256;
+constexpr int kTopParts = 16;
+
+__global__ __launch_bounds__(kJoinNT) void top_join(TopArgs a) {
+  __shared__ uint64_t list[kTopParts * 256];
+  const int tid = threadIdx.x;
+  const int k = a.k;
+  const int m = a.parts * k;
+  for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+    __syncthreads();
+    for (int i = tid; i < m; i += kJoinNT) list[i] = a.cand[row * m + i];
+    __syncthreads();
+    for (int i = tid; i < m; i += kJoinNT) {
+      const uint64_t c = list[i];
+      if (c == 0) continue;
+      const int own = i / k;
+      int rank = i - own * k;
+      for (int p = 0; p < a.parts && rank < k; ++p) {
+        if (p == own) continue;
+        int lo = 0, hi = k;                // entries [0, lo) are larger than c
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (list[p * k + mid] > c) lo = mid + 1;
+          else hi = mid;
+        }
+        rank += lo;
+      }
+      if (rank < k) {
+        a.values[row * k + rank] = key_value((uint32_t)(c >> 32));
+        a.ids[row * k + rank] = (int32_t)~(uint32_t)c;
+      }
+    }
+    if (tid == 0) {
+      float N = -INFINITY, S = 0.0f;
+      for (int p = 0; p < a.parts; ++p)
+        merge_ns_int(N, S, a.part[2 * (row * a.parts + p)], a.part[2 * (row * a.parts + p) + 1]);
+      a.lse[row] = (N == -INFINITY) ? __builtin_nanf("") : (N + log2f(S)) * kLn2;
+    }
+  }
+}
+
+}  // namespace
+
+int top_parts(int64_t T, int64_t V, int es) {
+  // a part of at least 4096 chunks, while the rows do not fill the device twice
+  const int64_t most = std::min<int64_t>(kTopParts, V * es / (16 * 4096));
+  const int64_t want = T > 0 ? 512 / T : 1;
+  return (int)std::max<int64_t>(1, std::min(most, want));
+}
+
+hipError_t launch_top_logits(const TopArgs& a, bool bf16, hipStream_t st) {
+  constexpr int NT = 512;
+  const int64_t items = (int64_t)a.T * a.parts;
+  const int64_t grid = std::min<int64_t>(items, kLaunchThreads / NT);
+  if (bf16) top_rows<uint16_t, NT><<<dim3((unsigned)grid), NT, 0, st>>>(a);
+  else top_rows<float, NT><<<dim3((unsigned)grid), NT, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && a.parts > 1) {
+    const int64_t g = std::min<int64_t>(a.T, kLaunchThreads / kJoinNT);
+    top_join<<<dim3((unsigned)g), kJoinNT, 0, st>>>(a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace dppo

@@ -1,0 +1,107 @@
+"""top_logits against the 64-bit oracle."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2605_12070_amd as P
+from operator_helpers import DEV, LSE, near, rows, values_of
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def check(z, k, tau=1.0):
+    r = P.top_logits(z, k, temperature=tau)
+    torch.cuda.synchronize()
+    v, i, lse = oracle.top_logits(values_of(z), k, tau)
+    assert r.values.dtype == torch.float32 and r.ids.dtype == torch.int32
+    assert np.array_equal(r.ids.cpu().numpy(), i), "ids"
+    assert np.array_equal(r.values.cpu().double().numpy(), v, equal_nan=True), "values"
+    near(r.lse.cpu().numpy(), lse, LSE * np.maximum(1, np.abs(np.nan_to_num(lse))), "lse")
+    return r
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,V,k", [
+    (1, 1, 1), (3, 2, 2), (5, 7, 7), (2, 9, 1), (4, 64, 64), (3, 100, 33), (7, 255, 255), (2, 256, 256),
+    (5, 257, 256), (6, 1000, 20), (3, 2055, 256), (3, 2110, 256), (2, 4096, 256), (4, 5001, 128),
+    (9, 8191, 17), (3, 16384, 1), (3, 32769, 64), (2, 50257, 128), (2, 151937, 256), (1, 262144, 64),
+    (600, 4100, 8), (2, 300001, 100),
+])
+def test_random_rows(dtype, T, V, k):
+    print(f"[case] top {dtype} T={T} V={V} k={k}", flush=True)
+    check(rows(T, V, dtype, seed=T + V + k), k, tau=1.0 if V % 2 else 0.7)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("offset", [0, 1, 3, 5])
+@pytest.mark.parametrize("ld", [1203, 1208])
+def test_strides_and_offsets(dtype, offset, ld):
+    print(f"[case] top {dtype} offset={offset} ld={ld}", flush=True)
+    check(rows(6, 1201, dtype, seed=5, ld=ld, offset=offset), 50)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [300, 9000, 40000, 151936])
+@pytest.mark.parametrize("kind", ["equal", "two", "sorted", "reversed", "few", "none", "lowest", "zeros"])
+def test_ties_and_orders(dtype, V, kind):
+    print(f"[case] top {dtype} V={V} {kind}", flush=True)
+    z = rows(3, V, dtype, seed=V)
+    if kind == "equal":
+        z.fill_(1.5)
+    elif kind == "two":                      # far more equal values than k
+        z.copy_((torch.rand(3, V, generator=torch.Generator().manual_seed(1)) < 0.5).to(dtype) * 2)
+    elif kind in ("sorted", "reversed"):
+        z.copy_(torch.sort(z.float(), dim=1, descending=kind == "reversed").values.to(dtype))
+    elif kind == "few":                      # a constrained step: most of the vocabulary masked
+        keep = torch.zeros(V, dtype=torch.bool, device=DEV)
+        keep[torch.randperm(V, generator=torch.Generator().manual_seed(2))[:30].to(DEV)] = True
+        z.masked_fill_(~keep, -float("inf"))
+    elif kind == "none":
+        z.fill_(-float("inf"))
+    elif kind == "lowest":                   # masked with the type's lowest value
+        z[:, 17:].fill_(torch.finfo(dtype).min)
+    else:
+        z.zero_()
+        z[:, ::2] = -0.0
+    for k in (1, 64, 256):
+        check(z, k)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [500, 30001])
+def test_non_finite(dtype, V):
+    print(f"[case] top {dtype} V={V} non-finite", flush=True)
+    z = rows(5, V, dtype, seed=9)
+    nan = torch.tensor([0x7FC0 if dtype == BF else 0x7FC00000]).to(torch.int16 if dtype == BF else torch.int32)
+    z[0, 5] = float("inf")
+    z[1, V - 1] = float("nan")
+    z[2, 3] = float("nan")
+    z[2, 400] = float("inf")
+    z[2, 7] = -float("inf")
+    ints = z.view(nan.dtype)
+    ints[3, 44] = ints[1, V - 1] | torch.iinfo(nan.dtype).min      # a NaN with its sign bit set
+    check(z, 40)
+
+
+def test_empty_batch_and_streams():
+    r = P.top_logits(torch.empty(0, 100, device=DEV), 5)
+    assert r.values.shape == (0, 5) and r.lse.shape == (0,)
+    z = rows(300, 20000, BF, seed=4)
+    want = check(z, 32)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = P.top_logits(z, 32)
+    s.synchronize()
+    for a, b in ((got.values, want.values), (got.ids, want.ids), (got.lse, want.lse)):
+        assert torch.equal(a, b)
+
+
+def test_the_same_bits_again():
+    z = rows(64, 50000, F32, seed=6)
+    a = P.top_logits(z, 256)
+    for _ in range(3):
+        b = P.top_logits(z, 256)
+        assert torch.equal(a.values, b.values) and torch.equal(a.ids, b.ids) and torch.equal(a.lse, b.lse)
