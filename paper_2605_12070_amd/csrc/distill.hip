@@ -54,20 +54,10 @@ struct RecordMath {    // one row at a time, between two barriers
   float w, lse2;
 };
 
-__device__ __forceinline__ double wave_sum_f64(double v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
-}
-__device__ __forceinline__ double wave_max_f64(double v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v = fmax(v, __shfl_xor(v, off, 64));
-  return v;
-}
-
 // The record's part of a row, by one wave: lane holds entries lane, lane + 64, ... N, S: the sum of
 // exponentials outside the record (2^N S, in log2 units). Everything an entry needs waits in LDS and
-// the loops are not unrolled: next to a row in registers there is no room for more.
+// the loops are not unrolled, and what all lanes share sits in scalar registers: next to a row in
+// vector registers there is no room for more.
 template <class Rec>
 __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, float scale, float N, float S,
                                             Rec& rec, RecordMath& m) {
@@ -81,8 +71,8 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
     tm = fmax(tm, (double)m.value[j] * a.t2e);
     zm = fmax(zm, (double)m.z[j] * zl);
   }
-  zm = wave_max_f64(zm);
-  tm = wave_max_f64(tm);
+  zm = wave_uniform(wave_max_f64(zm));
+  tm = wave_uniform(wave_max_f64(tm));
   const double zs = zm == -INFINITY ? 0.0 : zm;
   // the sums of exponentials around the maxima
   double st = 0.0, sq = 0.0;
@@ -92,17 +82,17 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
     if (tj != -INFINITY) st += exp2_f64(tj - tm);
     if (!rec.again[j]) sq += exp2_f64((double)m.z[j] * zl - zs);
   }
-  sq = wave_sum_f64(sq);
+  sq = wave_uniform(wave_sum_f64(sq));
   double c;
   if (a.tlse) {
     c = (double)a.tlse[row] * kLog2eF64;
   } else {
-    st = wave_sum_f64(st);
-    c = st == 0.0 ? 0.0 : tm + log2_f64(st);   // 0: an empty record, or one of -inf alone
+    st = wave_uniform(wave_sum_f64(st));
+    c = st == 0.0 ? 0.0 : wave_uniform(tm + log2_f64(st));   // 0: an empty record, or one of -inf alone
   }
-  const double rest = N == -INFINITY ? 0.0 : (double)S * exp2_f64((double)N - zs);
+  const double rest = wave_uniform(N == -INFINITY ? 0.0 : (double)S * exp2_f64((double)N - zs));
   const double total = sq + rest;
-  const double lse2 = zm == -INFINITY ? (double)__builtin_nanf("") : zs + log2_f64(total);
+  const double lse2 = zm == -INFINITY ? (double)__builtin_nanf("") : wave_uniform(zs + log2_f64(total));
   double l = 0.0, P = 0.0, Q = 0.0;
 #pragma unroll 1
   for (int j = lane; j < k; j += 64) {
@@ -116,11 +106,11 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
     m.p[j] = p;
     m.q[j] = q;
   }
-  l = wave_sum_f64(l);
-  P = wave_sum_f64(P);
+  l = wave_uniform(wave_sum_f64(l));
+  P = wave_uniform(wave_sum_f64(P));
   double f = P, g = P;
   if (a.tlse) {
-    Q = wave_sum_f64(Q);
+    Q = wave_uniform(wave_sum_f64(Q));
     const double Pt = 1.0 - P > 0.0 ? 1.0 - P : 0.0;
     const double Qt = fmax(rest / total, kTailFloor);
     if (Pt > 0.0) l += Pt * log2_f64(Pt / Qt) * kLn2F64;
@@ -149,9 +139,7 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
 template <typename Tin, int NT, int NC, int KS>
 __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
-  constexpr int P = NT * NC;               // chunks of a row in registers
   constexpr int U = 4;                     // further chunks per thread in flight
-  constexpr int kOff = 0x7fffff00;
   __shared__ float red[2][2 * (NT / 64)];
   __shared__ Record<NT> recs[2];
   __shared__ RecordMath rm;
@@ -190,206 +178,196 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
     const int64_t next = row + gridDim.x;
     const bool next_valid = next < a.T && is_valid(next);
     Tin* drow = a.dlogits ? (Tin*)a.dlogits + row * a.ldd : nullptr;
-    if (!valid) {
-      if (drow) zero_row<Tin, NT>(drow, V);
-      if (tid == 0) {
-        a.loss_tok[row] = 0.0f;
-        a.flags[row] = 0;
-      }
-      load_row(next, next_valid);
-      valid = next_valid;
-      continue;
-    }
-    Record<NT>& rec = recs[parity];
     const Tin* zrow = (const Tin*)a.logits + row * a.ld;
     const RowSplit sp = split_row(zrow, V);
     const int nfull = sp.nfull;
     const bool edge = tid < sp.nedge;
     const int ei = sp.template entry<E>(tid);
-    // the record: thread j holds entry j and hands it to the thread that owns its token
-    int id = -1;
-    float tv = 0.0f, tz = 0.0f;
-    bool bad = false;
-    if (tid < a.k) {
-      id = a.tokens[row * a.k + tid];
-      tv = a.values[row * a.k + tid];
-      bad = id < -1 || id >= V;
-      id = bad ? -1 : id;
-      rec.id[tid] = id;
-      rec.again[tid] = 0;
-      if (id >= 0) {
-        tz = sizeof(Tin) == 2 ? bf16_to_f32(((const uint16_t*)zrow)[id]) : ((const float*)zrow)[id];
-        const int e = id - sp.lead;
-        const int owner = e >= 0 && e < nfull * E ? (e / E) % NT : (e < 0 ? id : id - nfull * E);
-        rec.next[tid] = (int16_t)atomicExch(&rec.head[owner], tid);
+    Record<NT>& rec = recs[parity];
+    bool good = valid;
+    float tv = -INFINITY, tz = -INFINITY;  // this thread's entry of the record: value, student's logit
+    if (valid) {
+      // thread j holds entry j and hands it to the thread that owns its token
+      bool bad = false;
+      if (tid < a.k) {
+        int id = a.tokens[row * a.k + tid];
+        bad = id < -1 || id >= V;
+        id = bad ? -1 : id;
+        rec.id[tid] = id;
+        rec.again[tid] = 0;
+        if (id >= 0) {
+          tv = a.values[row * a.k + tid];
+          tz = sizeof(Tin) == 2 ? bf16_to_f32(((const uint16_t*)zrow)[id]) : ((const float*)zrow)[id];
+          const int e = id - sp.lead;
+          const int owner = e >= 0 && e < nfull * E ? (e / E) % NT : (e < 0 ? id : id - nfull * E);
+          rec.next[tid] = (int16_t)atomicExch(&rec.head[owner], tid);
+        }
       }
-    }
-    if (tid == 0) rm.any_again = 0;
-    if (__syncthreads_or(bad)) {           // a token outside the vocabulary: the row counts as bad
-      rec.head[tid] = -1;
+      if (tid == 0) rm.any_again = 0;
+      good = !__syncthreads_or(bad);       // a token outside the vocabulary makes the row bad
       parity ^= 1;
+    }
+    if (!good) {                           // uniform
+      if (valid) rec.head[tid] = -1;
       if (drow) zero_row<Tin, NT>(drow, V);
       if (tid == 0) {
         a.loss_tok[row] = 0.0f;
-        a.flags[row] = (uint8_t)(DPPO_FLAG_VALID | DPPO_FLAG_BAD_ID);
+        a.flags[row] = valid ? (uint8_t)(DPPO_FLAG_VALID | DPPO_FLAG_BAD_ID) : (uint8_t)0;
       }
-      load_row(next, next_valid);
-      valid = next_valid;
-      continue;
-    }
-    const int head = rec.head[tid];
-    uint32_t slots = 0;                    // bit s mod 32: a record's token lies in chunk slot s
-    bool edge_held = false;
-    for (int j = head; j >= 0; j = rec.next[j]) {
-      const int e = rec.id[j] - sp.lead;
-      if (e >= 0 && e < nfull * E) slots |= 1u << ((e / E / NT) & 31);
-      else edge_held = true;
-      for (int j2 = rec.next[j]; j2 >= 0; j2 = rec.next[j2])
-        if (rec.id[j2] == rec.id[j]) {
-          rec.again[j > j2 ? j : j2] = 1;
-          rm.any_again = 1;
-        }
-    }
-    // the record's entries of chunk idx (this thread's): f(j, entry of the chunk)
-    auto held = [&](int idx, auto&& f) {
+    } else {
+      const int head = rec.head[tid];
+      rec.head[tid] = -1;                  // the list stays reachable through `head`
+      uint32_t slots = 0;                  // bit s mod 32: a record's token lies in chunk slot s
+      bool edge_held = false;
       for (int j = head; j >= 0; j = rec.next[j]) {
-        const int e = rec.id[j] - sp.lead - idx * E;
-        if (e >= 0 && e < E) f(j, e);
-      }
-    };
-    float N = -INFINITY, S = 0.0f;
-    auto add = [&](float (&x)[E], int slot) {
-      if (slots >> (slot & 31) & 1u)
-        held(slot * NT + tid, [&](int, int e) {
-#pragma unroll
-          for (int i = 0; i < E; ++i) x[i] = i == e ? -INFINITY : x[i];
-        });
-      float cm = max3(x[0], x[1], x[2]);
-      if constexpr (E == 8) cm = max3(cm, max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
-      else cm = fmaxf(cm, x[3]);
-      const float nc = __builtin_ceilf(cm * L);
-      const float sh = (nc == -INFINITY) ? 0.0f : nc;
-      float s = 0.0f;
-#pragma unroll
-      for (int i = 0; i < E; ++i) s += exp2_hw(__builtin_fmaf(x[i], L, -sh));
-      merge_ns_int(N, S, nc, s);
-    };
-    const __amdgpu_buffer_rsrc_t rz = row_rsrc(zrow + sp.lead, nfull * 16);
-    // chunks past the registers first, so that their registers and the row's are not live together
-    if constexpr (KS > 0) {
-      for (int i0 = P + tid, s0 = NC; i0 < nfull; i0 += U * NT, s0 += U) {
-        u32x4 v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int idx = i0 + u * NT;
-          v[u] = buf_load16(rz, idx < nfull ? idx * 16 : kOff, 0);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (s0 + u - NC < KS) keep[(s0 + u - NC) * NT + tid] = v[u];
-          if (i0 + u * NT >= nfull) continue;
-          float x[E];
-          unpack(v[u], x);
-          add(x, s0 + u);
-        }
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      if (c * NT < nfull) {                // uniform
-        float x[E];
-        unpack(r[c], x);
-        if (c * NT + tid < nfull) add(x, c);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    float xe = -INFINITY;
-    if (edge) {
-      xe = sizeof(Tin) == 2 ? bf16_to_f32(((const uint16_t*)zrow)[ei]) : ((const float*)zrow)[ei];
-      bool own = false;
-      if (edge_held)
-        for (int j = head; j >= 0; j = rec.next[j]) own |= rec.id[j] == ei;
-      const float x = own ? -INFINITY : xe;
-      const float nc = __builtin_ceilf(x * L);
-      merge_ns_int(N, S, nc, nc == -INFINITY ? 0.0f : exp2_hw(__builtin_fmaf(x, L, -nc)));
-    }
-    if (tid < a.k) {
-      rm.value[tid] = id >= 0 ? tv : -INFINITY;
-      rm.z[tid] = id >= 0 ? tz : -INFINITY;
-    }
-    block_merge_ns_int<NT>(N, S, red[parity]);
-    if (tid < 64) record_math(a, row, scale * (a.tscale ? uload(a.tscale + row) : 1.0f), N, S, rec, rm);
-    if (tid == 0) a.flags[row] = (uint8_t)DPPO_FLAG_VALID;
-    parity ^= 1;
-    rec.head[tid] = -1;                    // this thread's list stays reachable through `head`
-    if (drow) {
-      __syncthreads();
-      const float w = rm.w, l2 = rm.lse2;
-      const __amdgpu_buffer_rsrc_t rd = row_rsrc(drow + sp.lead, nfull * 16);
-      const bool same = (((uintptr_t)drow - (uintptr_t)zrow) & 15) == 0;    // uniform
-      auto put = [&](const float (&x)[E], int slot) {
-        const int idx = slot * NT + tid;
-        float o[E];
-#pragma unroll
-        for (int i = 0; i < E; ++i) o[i] = w * exp2_hw(__builtin_fmaf(x[i], L, -l2));
-        if (slots >> (slot & 31) & 1u)
-          held(idx, [&](int j, int e) {
-            if (rec.again[j]) return;
-            const float gj = rec.grad[j];
-#pragma unroll
-            for (int i = 0; i < E; ++i) o[i] = i == e ? gj : o[i];
-          });
-        u32x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (sizeof(Tin) == 2) v[i] = pack_bf16(o[2 * i], o[2 * i + 1]);
-          else v[i] = __float_as_uint(o[i]);
-        }
-        if (same) {
-          buf_store16_nt(v, rd, idx < nfull ? idx * 16 : kOff, 0);
-        } else if (idx < nfull) {
-          Tin* d = drow + sp.lead + idx * E;
-#pragma unroll
-          for (int i = 0; i < E; ++i) {
-            if constexpr (sizeof(Tin) == 2) d[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
-            else d[i] = o[i];
+        const int e = rec.id[j] - sp.lead;
+        if (e >= 0 && e < nfull * E) slots |= 1u << ((e / E / NT) & 31);
+        else edge_held = true;
+        for (int j2 = rec.next[j]; j2 >= 0; j2 = rec.next[j2])
+          if (rec.id[j2] == rec.id[j]) {
+            rec.again[j > j2 ? j : j2] = 1;
+            rm.any_again = 1;
           }
+      }
+      // the record's entries of this thread's chunk of a slot: f(j, entry of the chunk). What depends
+      // on the slot is uniform here and below: a value per slot and thread would be kept in a
+      // register across the rows.
+      auto held = [&](int slot, auto&& f) {
+        for (int j = head; j >= 0; j = rec.next[j]) {
+          const int e = rec.id[j] - (sp.lead + slot * NT * E) - tid * E;
+          if (e >= 0 && e < E) f(j, e);
         }
       };
+      float N = -INFINITY, S = 0.0f;
+      auto add = [&](float (&x)[E], int slot) {
+        if (slots >> (slot & 31) & 1u)
+          held(slot, [&](int, int e) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if (c * NT < nfull) {
-          float x[E];
-          unpack(r[c], x);
-          put(x, c);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
+            for (int i = 0; i < E; ++i) x[i] = i == e ? -INFINITY : x[i];
+          });
+        float cm = max3(x[0], x[1], x[2]);
+        if constexpr (E == 8) cm = max3(cm, max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
+        else cm = fmaxf(cm, x[3]);
+        const float nc = __builtin_ceilf(cm * L);
+        const float sh = (nc == -INFINITY) ? 0.0f : nc;
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) s += exp2_hw(__builtin_fmaf(x[i], L, -sh));
+        merge_ns_int(N, S, nc, s);
+      };
+      const __amdgpu_buffer_rsrc_t rz = row_rsrc(zrow + sp.lead, nfull * 16);
+      // the chunks past the registers
       if constexpr (KS > 0) {
-        for (int i0 = P + tid, s0 = NC; i0 < nfull; i0 += U * NT, s0 += U) {
+        for (int s0 = NC; s0 * NT < nfull; s0 += U) {
           u32x4 v[U];
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int idx = i0 + u * NT;
-            if (s0 + u - NC < KS) v[u] = keep[(s0 + u - NC) * NT + tid];
-            else v[u] = buf_load16<kAuxLast>(rz, idx < nfull ? idx * 16 : kOff, 0);
-          }
+          for (int u = 0; u < U; ++u) v[u] = buf_load16(rz, tid * 16, (s0 + u) * NT * 16);
 #pragma unroll
           for (int u = 0; u < U; ++u) {
-            if (i0 + u * NT >= nfull) continue;
+            if (s0 + u - NC < KS) keep[(s0 + u - NC) * NT + tid] = v[u];
+            if (tid >= nfull - (s0 + u) * NT) continue;
             float x[E];
             unpack(v[u], x);
-            put(x, s0 + u);
+            add(x, s0 + u);
           }
         }
       }
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        if (c * NT < nfull) {              // uniform
+          float x[E];
+          unpack(r[c], x);
+          if (tid < nfull - c * NT) add(x, c);
+        }
+        // the words, not what was made of them, stay live until the gradient
+        asm volatile("" : "+v"(r[c][0]), "+v"(r[c][1]), "+v"(r[c][2]), "+v"(r[c][3]));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      float xe = -INFINITY;
       if (edge) {
-        float o = w * exp2_hw(__builtin_fmaf(xe, L, -l2));
+        xe = sizeof(Tin) == 2 ? bf16_to_f32(((const uint16_t*)zrow)[ei]) : ((const float*)zrow)[ei];
+        bool own = false;
         if (edge_held)
-          for (int j = head; j >= 0; j = rec.next[j])
-            if (rec.id[j] == ei && !rec.again[j]) o = rec.grad[j];
-        if constexpr (sizeof(Tin) == 2) drow[ei] = to_bf16(o);
-        else drow[ei] = o;
+          for (int j = head; j >= 0; j = rec.next[j]) own |= rec.id[j] == ei;
+        const float x = own ? -INFINITY : xe;
+        const float nc = __builtin_ceilf(x * L);
+        merge_ns_int(N, S, nc, nc == -INFINITY ? 0.0f : exp2_hw(__builtin_fmaf(x, L, -nc)));
+      }
+      if (tid < a.k) {
+        rm.value[tid] = tv;
+        rm.z[tid] = tz;
+      }
+      block_merge_ns_int<NT>(N, S, red[parity]);
+      if (tid < 64) record_math(a, row, scale * (a.tscale ? uload(a.tscale + row) : 1.0f), N, S, rec, rm);
+      if (tid == 0) a.flags[row] = (uint8_t)DPPO_FLAG_VALID;
+      if (drow) {
+        __syncthreads();
+        const float w = rm.w, l2 = rm.lse2;
+        const __amdgpu_buffer_rsrc_t rd = row_rsrc(drow + sp.lead, nfull * 16);
+        const bool same = (((uintptr_t)drow - (uintptr_t)zrow) & 15) == 0;    // uniform
+        auto put = [&](const float (&x)[E], int slot) {
+          float o[E];
+#pragma unroll
+          for (int i = 0; i < E; ++i) o[i] = w * exp2_hw(__builtin_fmaf(x[i], L, -l2));
+          if (slots >> (slot & 31) & 1u)
+            held(slot, [&](int j, int e) {
+              if (rec.again[j]) return;
+              const float gj = rec.grad[j];
+#pragma unroll
+              for (int i = 0; i < E; ++i) o[i] = i == e ? gj : o[i];
+            });
+          u32x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(Tin) == 2) v[i] = pack_bf16(o[2 * i], o[2 * i + 1]);
+            else v[i] = __float_as_uint(o[i]);
+          }
+          if (same) {
+            buf_store16_nt(v, rd, tid * 16, slot * NT * 16);   // dropped past the row
+          } else if (tid < nfull - slot * NT) {
+            // dlogits at another offset within 16 bytes: entry by entry
+            Tin* d = drow + (sp.lead + slot * NT * E) + tid * E;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+              if constexpr (sizeof(Tin) == 2) d[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+              else d[i] = __uint_as_float(v[i]);
+            }
+          }
+        };
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          if (c * NT < nfull) {
+            float x[E];
+            unpack(r[c], x);
+            put(x, c);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (KS > 0) {
+          for (int s0 = NC; s0 * NT < nfull; s0 += U) {
+            u32x4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              if (s0 + u - NC < KS) v[u] = keep[(s0 + u - NC) * NT + tid];
+              else v[u] = buf_load16<kAuxLast>(rz, tid * 16, (s0 + u) * NT * 16);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              if ((s0 + u) * NT >= nfull) continue;
+              float x[E];
+              unpack(v[u], x);
+              put(x, s0 + u);
+            }
+          }
+        }
+        if (edge) {
+          float o = w * exp2_hw(__builtin_fmaf(xe, L, -l2));
+          if (edge_held)
+            for (int j = head; j >= 0; j = rec.next[j])
+              if (rec.id[j] == ei && !rec.again[j]) o = rec.grad[j];
+          if constexpr (sizeof(Tin) == 2) drow[ei] = to_bf16(o);
+          else drow[ei] = o;
+        }
       }
     }
     load_row(next, next_valid);

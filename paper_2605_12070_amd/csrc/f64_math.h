@@ -3,25 +3,34 @@
 
 #include <hip/hip_runtime.h>
 
+#include "dppo_device.h"
+
 namespace dppo {
 
 constexpr double kLn2F64 = 0.69314718055994530942;
 constexpr double kLog2eF64 = 1.44269504088896340736;
 
+// p * f + c with the constant in a scalar register: left to itself the compiler keeps the polynomial's
+// constants in vector registers (18 of them) and copies each before it is accumulated upon.
+__device__ __forceinline__ double fma_const(double p, double f, double c) {
+  double r;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(p), "v"(f), "s"(c));
+  return r;
+}
+
 // 2^f for |f| <= 1/2: the polynomial of degree 9 through 2^f at the ten Chebyshev nodes of the
-// interval, relative error 1.9e-14 (ten fused multiply-adds, which run at the 32-bit rate on this
+// interval, relative error 1.9e-14 (fused multiply-adds, which run at the 32-bit rate on this
 // device).
 __device__ __forceinline__ double exp2_poly(double f) {
-  double p = 1.0205905413765595e-07;
-  p = __builtin_fma(p, f, 1.325964524488711e-06);
-  p = __builtin_fma(p, f, 1.5252672924850737e-05);
-  p = __builtin_fma(p, f, 0.0001540343375125101);
-  p = __builtin_fma(p, f, 0.0013333558200794592);
-  p = __builtin_fma(p, f, 0.009618129193934313);
-  p = __builtin_fma(p, f, 0.05550410866465167);
-  p = __builtin_fma(p, f, 0.2402265069564034);
-  p = __builtin_fma(p, f, 0.6931471805599462);
-  return __builtin_fma(p, f, 1.0000000000000135);
+  double p = fma_const(f, 1.0205905413765595e-07, 1.325964524488711e-06);
+  p = fma_const(p, f, 1.5252672924850737e-05);
+  p = fma_const(p, f, 0.0001540343375125101);
+  p = fma_const(p, f, 0.0013333558200794592);
+  p = fma_const(p, f, 0.009618129193934313);
+  p = fma_const(p, f, 0.05550410866465167);
+  p = fma_const(p, f, 0.2402265069564034);
+  p = fma_const(p, f, 0.6931471805599462);
+  return fma_const(p, f, 1.0000000000000135);
 }
 
 // 2^x; 0 below 2^-1100 (-inf included), NaN for NaN and +inf.
@@ -37,6 +46,45 @@ __device__ __forceinline__ double log2_f64(double x) {
   const double y = (double)log2f((float)x);
   const double e = __builtin_fma(x, exp2_f64(-y), -1.0);
   return y + e * (1.0 - 0.5 * e) * kLog2eF64;
+}
+
+// Wave-wide sum and maximum in 64 bits; every lane returns the same bits (a fixed tree of DPP moves
+// and permlane swaps, as the 32-bit ones).
+__device__ __forceinline__ double f64_of(uint32_t lo, uint32_t hi) {
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return f64_of(__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false),
+                __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, false));
+}
+template <class F>
+__device__ __forceinline__ double wave_fold_f64(double v, F&& f) {
+  v = f(v, dpp_d<0xB1>(v));    // quad_perm [1,0,3,2]
+  v = f(v, dpp_d<0x4E>(v));    // quad_perm [2,3,0,1]
+  v = f(v, dpp_d<0x141>(v));   // row_half_mirror
+  v = f(v, dpp_d<0x140>(v));   // row_mirror
+  uint64_t u = __builtin_bit_cast(uint64_t, v);
+  auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+  auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  v = f(f64_of(lo[0], hi[0]), f64_of(lo[1], hi[1]));
+  u = __builtin_bit_cast(uint64_t, v);
+  lo = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+  hi = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  return f(f64_of(lo[0], hi[0]), f64_of(lo[1], hi[1]));
+}
+__device__ __forceinline__ double wave_sum_f64(double v) {
+  return wave_fold_f64(v, [](double a, double b) { return a + b; });
+}
+__device__ __forceinline__ double wave_max_f64(double v) {
+  return wave_fold_f64(v, [](double a, double b) { return fmax(a, b); });
+}
+// A value that every lane of the wave holds, in scalar registers.
+__device__ __forceinline__ double wave_uniform(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return f64_of((uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u),
+                (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32)));
 }
 
 }  // namespace dppo
