@@ -27,6 +27,7 @@ constexpr int kStatsNT = 256;
 constexpr int kCellNT = 256;
 constexpr int kPickNT = 256;
 constexpr int kMaxParts = 16;
+constexpr int64_t kStatsRows = 512;   // rows of a launch of the statistics
 
 template <typename Tin>
 __device__ __forceinline__ float entry_value(const Tin* p, int64_t i) {
@@ -71,89 +72,6 @@ __device__ __forceinline__ void join(double& m, double& s, double m2, double s2,
   m = M;
 }
 
-// One part of one row's statistics per workgroup; positions outermost, so that the rows every
-// sequence needs come first.
-template <typename Tin>
-__global__ __launch_bounds__(kStatsNT) void verify_stats(VerifyArgs a) {
-  constexpr int E = 16 / (int)sizeof(Tin);
-  constexpr int NT = kStatsNT;
-  constexpr int U = 4;
-  constexpr int NW = NT / 64;
-  constexpr int kOff = 0x7fffff00;
-  __shared__ double red[2 * NW];
-  const int tid = threadIdx.x;
-  const int kinds = a.draft ? 2 : 1;
-  const int64_t items = (int64_t)(a.D + 1) * a.B * kinds * a.parts;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int part = (int)(item % a.parts);
-    const int64_t rest = item / a.parts;
-    const int kind = (int)(rest % kinds);
-    const int64_t at = rest / kinds;                 // i * B + b
-    const int b = (int)(at % a.B);
-    const int i = (int)(at / a.B);
-    if (i + kind > drafts_of(a, b)) continue;        // uniform: not a row of this sequence
-    const Tin* z = kind ? draft_row<Tin>(a, b, i) : target_row<Tin>(a, b, i);
-    const RowSplit sp = split_row(z, a.V);
-    const int c0 = (int)((int64_t)sp.nfull * part / a.parts);
-    const int n = (int)((int64_t)sp.nfull * (part + 1) / a.parts) - c0;
-    const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + sp.lead + (int64_t)c0 * E, n * 16);
-    float m = -INFINITY;                             // this thread's maximum
-    double s = 0.0, ref = 0.0;                       // ref: m, or 0 while that is -inf
-    auto add = [&](const auto& x, float cm) {
-      if (cm > m) {
-        s *= exp2_f64(((double)m - (double)cm) * a.t2e);
-        m = cm;
-        ref = cm;
-      }
-      // the difference first: a product with a far logit (a mask of the type's lowest value) has no
-      // fraction left
-#pragma unroll
-      for (int j = 0; j < (int)(sizeof(x) / 4); ++j) s += exp2_f64(((double)x[j] - ref) * a.t2e);
-    };
-    u32x4 r[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) r[u] = buf_load16<kAuxLast>(rz, u * NT + tid < n ? (u * NT + tid) * 16 : kOff, 0);
-    if (part == 0 && tid < sp.nedge) {
-      const float x[1] = {entry_value(z, sp.entry<E>(tid))};
-      add(x, x[0]);
-    }
-    for (int base = 0; base < n; base += U * NT) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = base + u * NT + tid;
-        float x[E];
-        unpack<Tin>(r[u], x);
-        r[u] = buf_load16<kAuxLast>(rz, c + U * NT < n ? (c + U * NT) * 16 : kOff, 0);
-        if (c < n) {
-          float cm = max3(x[0], x[1], x[2]);
-          if constexpr (E == 8) cm = max3(cm, max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
-          else cm = fmaxf(cm, x[3]);
-          add(x, cm);
-        }
-      }
-    }
-    double md = m;
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-      const double m2 = __shfl_xor(md, off, 64);
-      const double s2 = __shfl_xor(s, off, 64);
-      join(md, s, m2, s2, a.t2e);
-    }
-    __syncthreads();                                 // the last item's partials are read
-    if ((tid & 63) == 0) {
-      red[tid >> 6] = md;
-      red[NW + (tid >> 6)] = s;
-    }
-    __syncthreads();
-    if (tid == 0) {
-      for (int w = 1; w < NW; ++w) join(md, s, red[w], red[NW + w], a.t2e);
-      double* out = a.stats + ((at * 2 + kind) * a.parts + part) * 2;
-      out[0] = md;
-      out[1] = s;
-    }
-  }
-}
-
 // A row's normaliser from its parts; NaN for a row that cannot be evaluated.
 __device__ __forceinline__ VerifyNorm row_norm(const VerifyArgs& a, int64_t b, int64_t i, int kind) {
   const double* st = a.stats + ((i * a.B + b) * 2 + kind) * a.parts * 2;
@@ -166,12 +84,12 @@ __device__ __forceinline__ double log2_prob(const VerifyArgs& a, const VerifyNor
   return __builtin_fma((double)z - n.m, a.t2e, -n.log2s);
 }
 
-// Where sequence b stops, by one wave; every lane returns the same. With `write`, the accepted drafts
-// and their log-probs go to the outputs.
+// Where sequence b stops among its first n drafts, by one wave; every lane returns the same. With
+// `write`, the accepted drafts and their log-probs go to the outputs. (Lanes behind the stop may read
+// statistics that were never computed; the first lane that stops decides.)
 template <typename Tin>
-__device__ __forceinline__ VerifyDraw decide(const VerifyArgs& a, int b, bool write) {
+__device__ __forceinline__ VerifyDraw decide(const VerifyArgs& a, int b, int n, bool write) {
   const int lane = threadIdx.x & 63;
-  const int n = drafts_of(a, b);
   VerifyDraw d{};
   d.pos = n;
   d.mode = kDrawTarget;
@@ -208,9 +126,101 @@ __device__ __forceinline__ VerifyDraw decide(const VerifyArgs& a, int b, bool wr
       return d;
     }
   }
-  d.p = row_norm(a, b, n, 0);
-  if (d.p.log2s != d.p.log2s) d.mode = kDrawBad;
   return d;
+}
+
+// One part of one row's statistics per workgroup, for the positions [i0, i1); positions outermost.
+// Sequences that stop before i0 (their statistics are complete: an earlier launch) are skipped.
+template <typename Tin>
+__global__ __launch_bounds__(kStatsNT) void verify_stats(VerifyArgs a, int i0, int i1) {
+  constexpr int E = 16 / (int)sizeof(Tin);
+  constexpr int NT = kStatsNT;
+  constexpr int U = 4;
+  constexpr int NW = NT / 64;
+  constexpr int kOff = 0x7fffff00;
+  __shared__ double red[2 * NW];
+  __shared__ int alive;
+  const int tid = threadIdx.x;
+  const int kinds = a.draft ? 2 : 1;
+  const int64_t items = (int64_t)(i1 - i0) * a.B * kinds * a.parts;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int part = (int)(item % a.parts);
+    const int64_t rest = item / a.parts;
+    const int kind = (int)(rest % kinds);
+    const int b = (int)((rest / kinds) % a.B);
+    const int i = i0 + (int)((rest / kinds) / a.B);
+    const int drafts = drafts_of(a, b);
+    if (i + kind > drafts) continue;                 // uniform: not a row of this sequence
+    const int64_t at = (int64_t)i * a.B + b;
+    const Tin* z = kind ? draft_row<Tin>(a, b, i) : target_row<Tin>(a, b, i);
+    const RowSplit sp = split_row(z, a.V);
+    const int c0 = (int)((int64_t)sp.nfull * part / a.parts);
+    const int n = (int)((int64_t)sp.nfull * (part + 1) / a.parts) - c0;
+    const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + sp.lead + (int64_t)c0 * E, n * 16);
+    u32x4 r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u] = buf_load16<kAuxLast>(rz, u * NT + tid < n ? (u * NT + tid) * 16 : kOff, 0);
+    if (i0 > 0) {
+      __syncthreads();                               // the last item's flag is read
+      if (tid < 64) {
+        const bool on = decide<Tin>(a, b, i0, false).mode == kDrawTarget;
+        if (tid == 0) alive = on;
+      }
+      __syncthreads();
+      if (!alive) continue;
+    }
+    float m = -INFINITY;                             // this thread's maximum
+    double s = 0.0, ref = 0.0;                       // ref: m, or 0 while that is -inf
+    auto add = [&](const auto& x, float cm) {
+      if (cm > m) {
+        s *= exp2_f64(((double)m - (double)cm) * a.t2e);
+        m = cm;
+        ref = cm;
+      }
+      // the difference first: a product with a far logit (a mask of the type's lowest value) has no
+      // fraction left
+#pragma unroll
+      for (int j = 0; j < (int)(sizeof(x) / 4); ++j) s += exp2_f64(((double)x[j] - ref) * a.t2e);
+    };
+    if (part == 0 && tid < sp.nedge) {
+      const float x[1] = {entry_value(z, sp.entry<E>(tid))};
+      add(x, x[0]);
+    }
+    for (int base = 0; base < n; base += U * NT) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = base + u * NT + tid;
+        float x[E];
+        unpack<Tin>(r[u], x);
+        r[u] = buf_load16<kAuxLast>(rz, c + U * NT < n ? (c + U * NT) * 16 : kOff, 0);
+        if (c < n) {
+          float cm = max3(x[0], x[1], x[2]);
+          if constexpr (E == 8) cm = max3(cm, max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
+          else cm = fmaxf(cm, x[3]);
+          add(x, cm);
+        }
+      }
+    }
+    double md = m;
+    {
+      // the wave's maximum, then one exponential per thread (NaN sums stay NaN)
+      const double M = wave_max_f64(md);
+      s = wave_sum_f64(md == M ? s : s * exp2_f64((md - M) * a.t2e));
+      md = M;
+    }
+    __syncthreads();                                 // the last item's partials are read
+    if ((tid & 63) == 0) {
+      red[tid >> 6] = md;
+      red[NW + (tid >> 6)] = s;
+    }
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < NW; ++w) join(md, s, red[w], red[NW + w], a.t2e);
+      double* out = a.stats + ((at * 2 + kind) * a.parts + part) * 2;
+      out[0] = md;
+      out[1] = s;
+    }
+  }
 }
 
 // Weights of the E entries from entry e0 on (a whole chunk of the target's row).
@@ -285,9 +295,7 @@ __device__ __forceinline__ double cell_sum(const VerifyArgs& a, const VerifyDraw
   double s = 0.0;
 #pragma unroll
   for (int j = 0; j < E; ++j) s += w[j];
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off, 64);
-  return s;
+  return wave_sum_f64(s);
 }
 
 template <typename Tin>
@@ -299,7 +307,12 @@ __global__ __launch_bounds__(kCellNT) void verify_cells(VerifyArgs a) {
     const int part = (int)(item % a.draw_parts);
     __syncthreads();
     if (wave == 0) {
-      const VerifyDraw d = decide<Tin>(a, b, part == 0);
+      const int n = drafts_of(a, b);
+      VerifyDraw d = decide<Tin>(a, b, n, part == 0);
+      if (d.mode == kDrawTarget) {
+        d.p = row_norm(a, b, n, 0);
+        if (d.p.log2s != d.p.log2s) d.mode = kDrawBad;
+      }
       if (threadIdx.x == 0) {
         ds = d;
         if (part == 0) a.draw[b] = d;
@@ -325,7 +338,9 @@ template <typename Tin>
 __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int NT = kPickNT;
-  __shared__ double sums[NT];
+  constexpr int NW = NT / 64;
+  __shared__ double wsum[2][NW];
+  __shared__ double before_s;
   __shared__ int found_s, last_s;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -353,26 +368,32 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
     int mode = d.mode;
     const int run = (a.cells + NT - 1) / NT;          // cells per thread, consecutive
     const int r0 = min(tid * run, a.cells), r1 = min(r0 + run, a.cells);
-    double before = 0.0, total = 0.0;
+    double before = 0.0, total = 0.0;                // the cells before this thread's, and all of them
     for (int attempt = 0; attempt < 2; ++attempt) {
       double own = 0.0;
       for (int c = r0; c < r1; ++c) own += cell[c];
-      __syncthreads();
-      sums[tid] = own;
+      double incl = own;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const double o = __shfl_up(incl, off, 64);
+        if (lane >= off) incl += o;
+      }
+      if (lane == 63) wsum[attempt][tid >> 6] = incl;
       if (tid == 0) {
         found_s = a.cells;
         last_s = -1;
       }
       __syncthreads();
-      before = total = 0.0;
-      for (int t = 0; t < NT; ++t) {
-        if (t == tid) before = total;
-        total += sums[t];
+      total = 0.0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        if (w == tid >> 6) before = total + (incl - own);
+        total += wsum[attempt][w];
       }
       if (total > 0.0) break;                        // uniform
       // p - q has no positive part: the draw is from p (the sums again, in this workgroup)
       mode = kDrawTarget;
-      for (int c = tid >> 6; c < a.cells; c += NT / 64) {
+      for (int c = tid >> 6; c < a.cells; c += NW) {
         const double s = cell_sum(a, d, mode, p, q, x, sp, c);
         if (lane == 0) cell[c] = s;
       }
@@ -380,26 +401,29 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
       __syncthreads();
     }
     const double goal = (double)a.u_new[b] * total;
+    int hit_cell = a.cells;
+    double hit_before = before;
     {
       double c = before;
       for (int i = r0; i < r1; ++i) {
         const double w = cell[i];
         if (w > 0.0) atomicMax(&last_s, i);
-        c += w;
-        if (c > goal && w > 0.0) {
+        if (c + w > goal && w > 0.0) {
           atomicMin(&found_s, i);
+          hit_cell = i;
+          hit_before = c;
           break;
         }
+        c += w;
       }
     }
     __syncthreads();
     const int found = found_s < a.cells ? found_s : last_s;   // total > 0: some weight is positive
+    if (hit_cell == found) before_s = hit_before;             // one thread, if a cell was hit
+    __syncthreads();
     if (tid < 64 && found >= 0) {
-      // the running sum before the cell, in the order the runs were added
-      const int t0 = found / run;
-      double c = 0.0;
-      for (int t = 0; t < t0; ++t) c += sums[t];
-      for (int i = t0 * run; i < found; ++i) c += cell[i];
+      double c = before_s;                                    // no cell hit: not used, c > goal fails
+      if (found_s == a.cells) c = -INFINITY;
       const CellSpan s = cell_span<Tin>(sp, a.V, a.cells, found, lane);
       double w[E];
       span_weights(a, d, mode, p, q, x, s, w);
@@ -433,7 +457,7 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
                              : __builtin_nanf("");
       }
     }
-    __syncthreads();                                 // sums and found_s are read
+    __syncthreads();                                 // the sequence's LDS is read
   }
 }
 
@@ -442,8 +466,9 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
 int64_t verify_layout(VerifyArgs& a, int es, bool with_draft, void* workspace) {
   const int E = 16 / es;
   const int64_t chunks = a.V / E;
-  const int64_t rows = std::max<int64_t>(1, (int64_t)a.B * (a.D + 1 + (with_draft ? a.D : 0)));
-  // a part of two chunks per thread or more, while the rows do not fill the device
+  const int64_t per = (int64_t)a.B * (with_draft ? 2 : 1);
+  const int64_t rows = std::max<int64_t>(1, std::min<int64_t>(per * (a.D + 1), std::max<int64_t>(per, kStatsRows)));
+  // a part of two chunks per thread or more, while a launch's rows do not fill the device
   a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxParts, 2048 / rows, chunks / (2 * kStatsNT)}));
   a.cells = (int)((chunks + 63) / 64 + 2);
   a.draw_parts = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / std::max(a.B, 1), a.cells / 8));
@@ -460,16 +485,22 @@ int64_t verify_layout(VerifyArgs& a, int es, bool with_draft, void* workspace) {
 }
 
 hipError_t launch_verify(const VerifyArgs& a, bool bf16, hipStream_t st) {
-  const int64_t items = (int64_t)(a.D + 1) * a.B * (a.draft ? 2 : 1) * a.parts;
-  const unsigned g1 = (unsigned)std::min<int64_t>(items, kLaunchThreads / kStatsNT);
   const unsigned g2 = (unsigned)std::min<int64_t>((int64_t)a.B * a.draw_parts, kLaunchThreads / kCellNT);
   const unsigned g3 = (unsigned)std::min<int64_t>(a.B, kLaunchThreads / kPickNT);
+  // Positions in groups that fill the device; a sequence that an earlier group stops is not read on.
+  // At most eight launches however many drafts there are.
+  const int64_t per = (int64_t)a.B * (a.draft ? 2 : 1);
+  const int group = (int)std::max<int64_t>((kStatsRows + per - 1) / per, (a.D + 1 + 7) / 8);
+  for (int i0 = 0; i0 <= a.D; i0 += group) {
+    const int i1 = std::min(a.D + 1, i0 + group);
+    const unsigned g1 = (unsigned)std::min<int64_t>((i1 - i0) * per * a.parts, kLaunchThreads / kStatsNT);
+    if (bf16) verify_stats<uint16_t><<<g1, kStatsNT, 0, st>>>(a, i0, i1);
+    else verify_stats<float><<<g1, kStatsNT, 0, st>>>(a, i0, i1);
+  }
   if (bf16) {
-    verify_stats<uint16_t><<<g1, kStatsNT, 0, st>>>(a);
     verify_cells<uint16_t><<<g2, kCellNT, 0, st>>>(a);
     verify_pick<uint16_t><<<g3, kPickNT, 0, st>>>(a);
   } else {
-    verify_stats<float><<<g1, kStatsNT, 0, st>>>(a);
     verify_cells<float><<<g2, kCellNT, 0, st>>>(a);
     verify_pick<float><<<g3, kPickNT, 0, st>>>(a);
   }
