@@ -481,7 +481,7 @@ dppo_status dppo_scale_to_bf16(const float* src, int64_t n, const float* g, void
  *
  *  logits       as for logprob_fwd; V <= 2^28.
  *  k            1 <= k <= min(V, DPPO_MAX_TOP).
- *  temperature  tau > 0, finite, with 1 / tau finite.
+ *  temperature  tau in [1e-6, 1e6].
  *  values_out   [T, k] float32, the logits themselves (not divided by tau; -0 is returned as 0).
  *  ids_out      [T, k] int32, their places. Equal values come lowest id first; a NaN counts as
  *               larger than every number.
@@ -519,7 +519,7 @@ int64_t top_logits_workspace_bytes(int32_t dtype, int64_t T, int64_t V, int32_t 
  *                   shorter than k), whose value is not used. 1 <= k <= DPPO_MAX_TOP.
  *  teacher_lse      [T] float32 or NULL.
  *  loss_mask, token_scale, scale_mode, loss_scale  as in decoupled_ppo_loss_fwd_bwd.
- *  temperature      tau > 0, finite, with 1 / tau finite.
+ *  temperature      tau in [1e-6, 1e6].
  *  kl_out           [T] float32: l_t (0 on masked and bad rows).
  *  loss_out         [1] float32, summed as in decoupled_ppo_loss_fwd_bwd.
  *  flags_out        [T] uint8: DPPO_FLAG_VALID, DPPO_FLAG_BAD_ID.
@@ -550,15 +550,17 @@ dppo_status distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t T, i
  *  draft       [B, D, V] of `dtype` with strides draft_seq, draft_row: the draft model's logits; NULL:
  *              drafts without a distribution (greedy, n-gram), q_i = 1 at x_i and 0 elsewhere.
  *  draft_ids   [B, D] int64.   num_drafts [B] int32 or NULL (all D); values are held in [0, D].
- *  accept_u    [B, D] float32, sample_u [B] float32, in [0, 1).
+ *  accept_u    [B, D] float32, sample_u [B] float32, in [0, 1).   temperature in [1e-6, 1e6].
  *  B >= 0, 0 <= D <= 1024 (accept_u and draft_ids may be NULL with D = 0), 1 <= V <= 2^28.
  *  accepted_out [B] int32: a.
  *  tokens_out   [B, D + 1] int64: the accepted drafts, the drawn token, then -1.
  *  logp_out     [B, D + 1] float32: log p_i of the emitted tokens (log mu_old of the loss calls), then 0.
  *  workspace    device buffer of verify_drafts_workspace_bytes bytes or more, 16-byte aligned.
- * The decisions and the draw are computed in 64 bits. Rows behind a are not part of the result. A
- * sequence that reaches a draft id outside [0, V), or a row holding NaN or +inf or only -inf, ends
- * there: its drawn token is -1, with log-prob NaN.
+ * The decisions and the draw are those of 64-bit arithmetic (a weight is good to 5e-12; weights below
+ * 1e-280, and a residual below 1e-12 in all, count as 0); the accepted drafts' log-probs are as exact
+ * as logprob_fwd's. Rows behind a are not part of the result. A sequence that reaches a draft id
+ * outside [0, V), or a row holding NaN or +inf or only -inf, ends there: its drawn token is -1, with
+ * log-prob NaN.
  */
 dppo_status verify_drafts(const void* target, int64_t target_seq, int64_t target_row, const void* draft,
                           int64_t draft_seq, int64_t draft_row, int32_t dtype, int64_t B, int64_t D,

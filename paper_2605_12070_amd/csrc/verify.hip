@@ -2,15 +2,19 @@
 // numbers: which drafts are accepted, the token drawn behind them, and the log-probs of both.
 //
 // Accepting compares u q(x) with p(x), and the draw finds where a running sum passes u times its
-// total: both turn on the last bits of sums over the vocabulary, and another summation order would
-// now and then emit another token. So probabilities, sums and running sums are held in 64 bits, with
-// exponentials good to 2e-14; fused multiply-adds in 64 bits run at the 32-bit rate here, and an
-// exponential costs about twice what the 32-bit path with the transcendental unit does.
-//
-// Three kernels: the maximum and sum of exponentials of every row that a sequence may need, in parts
-// where rows are few; the weights' sums over cells of 64 chunks of the row each sequence draws from
-// (each workgroup first decides, from the rows' sums, where its sequence stops); and the draw: the
-// cell where the running sum passes, then the entry.
+// total. Both turn on the last bits of sums over the vocabulary, and a draw from V weights goes wrong
+// with a probability of about V times the running sums' error. So the draw's weights and sums are held
+// in 64 bits (exponentials good to 5e-12). That costs five times a 32-bit exponential, and is spent on
+// the one pair of rows that a sequence draws from:
+//   1. statistics: every row's sum of exponentials with 32-bit exponentials, an error of a few 1e-6
+//      that the row's size bounds. Positions come in groups; a sequence that an earlier group stops
+//      is not read on.
+//   2. cells: a workgroup finds where its sequence stops. An acceptance that lies within that bound is
+//      decided by exact sums over its two rows. Then the weights of the row drawn from are summed over
+//      cells of 64 chunks, in one pass that also sums p and q themselves: the weights max(p - q, 0) are
+//      formed with the 32-bit normalisers, and the exact ones that the pass yields correct their sums
+//      to first order (what changes sign within 1e-6 is second order, 1e-12).
+//   3. the draw: the cell where the corrected running sum passes, then the entry, from exact weights.
 #include "verify.h"
 
 #include <algorithm>
@@ -47,6 +51,12 @@ __device__ __forceinline__ void unpack(const W& r, float (&x)[16 / sizeof(Tin)])
     }
   }
 }
+template <int E>
+__device__ __forceinline__ float max_of(const float (&x)[E]) {
+  if constexpr (E == 8) return max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
+  else if constexpr (E == 4) return max3(max3(x[0], x[1], x[2]), x[3], x[3]);
+  else return x[0];
+}
 
 __device__ __forceinline__ int drafts_of(const VerifyArgs& a, int b) {
   if (!a.num) return a.D;
@@ -62,86 +72,97 @@ __device__ __forceinline__ const Tin* draft_row(const VerifyArgs& a, int64_t b, 
   return (const Tin*)a.draft + b * a.draft_seq + i * a.draft_row;
 }
 
-// Joins (maximum, sum of 2^((z - maximum) t2e)) pairs; maxima in the logits' units. A sum that is NaN
-// stays so.
-__device__ __forceinline__ void join(double& m, double& s, double m2, double s2, double t2e) {
-  const double M = fmax(m, m2);
-  const double fa = m == M ? 1.0 : exp2_f64((m - M) * t2e);
-  const double fb = m2 == M ? 1.0 : exp2_f64((m2 - M) * t2e);
-  s = s * fa + s2 * fb;
-  m = M;
+// ------------------------------------------------------------------ where a sequence stops
+// A row's sum of exponentials as the statistics have it: log2 of it, and a bound on its error. Far
+// rows (logits past 2^20 log2 units, infinite ones and rows of nothing else than -inf or the type's
+// lowest value among them) are left to exact arithmetic.
+struct RowNorm {
+  double lse2, err;
+  bool far, bad;
+};
+__device__ __forceinline__ RowNorm row_norm(const VerifyArgs& a, int64_t b, int64_t i, int kind) {
+  const VerifyPart* st = a.stats + ((i * a.B + b) * 2 + kind) * a.parts;
+  double n = -INFINITY, m = -INFINITY;
+  for (int p = 0; p < a.parts; ++p) {
+    n = fmax(n, st[p].n);
+    m = fmax(m, st[p].m);
+  }
+  double s = 0.0;
+  for (int p = 0; p < a.parts; ++p)
+    if (st[p].n != -INFINITY) s += st[p].s * exp2_f64(st[p].n - n);
+  RowNorm r;
+  r.far = !(fabs(m) * a.t2e < 1048576.0);
+  r.bad = !r.far && !(s > 0.0 && s < INFINITY);
+  r.lse2 = r.far || r.bad ? 0.0 : n + log2_f64(s);
+  // Terms: the exponential (2^-22) and a chunk's additions (2^-22); its argument's rounding, 2^-24 of
+  // log2 units below the maximum, which weighs at most log2(V) <= 28 over the row; the 32-bit log2(e) /
+  // temperature, 2^-25 of the logits that matter. In all below 2.7e-6 + |m t2e| 2^-24 of the sum.
+  r.err = 8e-6 + fabs(r.lse2) * 2.4e-7;
+  return r;
 }
 
-// A row's normaliser from its parts; NaN for a row that cannot be evaluated.
-__device__ __forceinline__ VerifyNorm row_norm(const VerifyArgs& a, int64_t b, int64_t i, int kind) {
-  const double* st = a.stats + ((i * a.B + b) * 2 + kind) * a.parts * 2;
-  double m = st[0], s = st[1];
-  for (int p = 1; p < a.parts; ++p) join(m, s, st[2 * p], st[2 * p + 1], a.t2e);
-  return {m, s > 0.0 && s < INFINITY && m < INFINITY ? log2_f64(s) : (double)__builtin_nanf("")};
-}
-// log2 of an entry's probability.
-__device__ __forceinline__ double log2_prob(const VerifyArgs& a, const VerifyNorm& n, float z) {
-  return __builtin_fma((double)z - n.m, a.t2e, -n.log2s);
-}
+enum Status { kAccept, kReject, kUnclear, kBadRow };
 
-// Where sequence b stops among its first n drafts, by one wave; every lane returns the same. With
-// `write`, the accepted drafts and their log-probs go to the outputs. (Lanes behind the stop may read
-// statistics that were never computed; the first lane that stops decides.)
+// The first of the drafts [i0, n) of sequence b that is not clearly accepted, by one wave: every lane
+// returns the same position (n if there is none) and its status. With `write`, the accepted drafts
+// and their log-probs go to the outputs. (Lanes behind that draft may read statistics that were
+// never computed; they decide nothing.)
+struct Stop {
+  int pos;
+  int status;
+};
 template <typename Tin>
-__device__ __forceinline__ VerifyDraw decide(const VerifyArgs& a, int b, int n, bool write) {
+__device__ __forceinline__ Stop first_stop(const VerifyArgs& a, int b, int i0, int n, bool write) {
   const int lane = threadIdx.x & 63;
-  VerifyDraw d{};
-  d.pos = n;
-  d.mode = kDrawTarget;
-  for (int i0 = 0; i0 < n; i0 += 64) {
+  for (; i0 < n; i0 += 64) {
     const int i = i0 + lane;
-    bool accept = true, bad = false;
-    VerifyNorm np{}, nq{};
+    int status = kAccept;
     float out = 0.0f;
     int64_t x = -1;
     if (i < n) {
       x = a.ids[(int64_t)b * a.D + i];
-      np = row_norm(a, b, i, 0);
-      if (a.draft) nq = row_norm(a, b, i, 1);
-      bad = x < 0 || x >= a.V || np.log2s != np.log2s || nq.log2s != nq.log2s;
-      accept = false;
-      if (!bad) {
-        const double lp = log2_prob(a, np, entry_value(target_row<Tin>(a, b, i), x));
-        const double q = a.draft ? exp2_f64(log2_prob(a, nq, entry_value(draft_row<Tin>(a, b, i), x))) : 1.0;
-        accept = (double)a.u[(int64_t)b * a.D + i] * q < exp2_f64(lp);
+      const RowNorm p = row_norm(a, b, i, 0);
+      RowNorm q{};
+      if (a.draft) q = row_norm(a, b, i, 1);
+      if (x < 0 || x >= a.V || p.bad || q.bad) {
+        status = kBadRow;
+      } else if (p.far || q.far) {
+        status = kUnclear;
+      } else {
+        const double lp = __builtin_fma((double)entry_value(target_row<Tin>(a, b, i), x), a.t2e, -p.lse2);
+        const double lq = a.draft ? __builtin_fma((double)entry_value(draft_row<Tin>(a, b, i), x), a.t2e, -q.lse2) : 0.0;
+        const double uq = (double)a.u[(int64_t)b * a.D + i] * exp2_f64(lq), pp = exp2_f64(lp);
+        const double mu = p.err + q.err;
+        status = uq * (1.0 + mu) < pp ? kAccept : (uq < pp * (1.0 + mu) ? kUnclear : kReject);
+        if (pp == 0.0) status = kReject;
         out = (float)(lp * kLn2F64);
       }
     }
-    const uint64_t stops = __ballot(!accept);
+    const uint64_t stops = __ballot(status != kAccept);
     const int stop = stops ? __builtin_ctzll(stops) : 64;
     if (write && i < n && lane < stop) {
       a.tokens[(int64_t)b * (a.D + 1) + i] = x;
       a.logp[(int64_t)b * (a.D + 1) + i] = out;
     }
-    if (stop < 64) {
-      d.pos = i0 + stop;
-      d.p = {__shfl(np.m, stop, 64), __shfl(np.log2s, stop, 64)};
-      d.q = {__shfl(nq.m, stop, 64), __shfl(nq.log2s, stop, 64)};
-      d.mode = __shfl((int)bad, stop, 64) ? kDrawBad : (a.draft ? kDrawResidual : kDrawWithout);
-      return d;
-    }
+    if (stop < 64) return {i0 + stop, __shfl(status, stop, 64)};
   }
-  return d;
+  return {n, kAccept};
 }
 
-// One part of one row's statistics per workgroup, for the positions [i0, i1); positions outermost.
-// Sequences that stop before i0 (their statistics are complete: an earlier launch) are skipped.
+// ------------------------------------------------------------------ statistics
+// One part of one row per workgroup, for the positions [i0, i1); positions outermost. Sequences that
+// clearly stop before i0 (whose statistics are complete: earlier launches) are skipped.
 template <typename Tin>
 __global__ __launch_bounds__(kStatsNT) void verify_stats(VerifyArgs a, int i0, int i1) {
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int NT = kStatsNT;
-  constexpr int U = 4;
+  constexpr int U = 8;
   constexpr int NW = NT / 64;
-  constexpr int kOff = 0x7fffff00;
-  __shared__ double red[2 * NW];
+  __shared__ double red[3 * NW];
   __shared__ int alive;
   const int tid = threadIdx.x;
   const int kinds = a.draft ? 2 : 1;
+  const float L = (float)a.t2e;
   const int64_t items = (int64_t)(i1 - i0) * a.B * kinds * a.parts;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int part = (int)(item % a.parts);
@@ -149,115 +170,137 @@ __global__ __launch_bounds__(kStatsNT) void verify_stats(VerifyArgs a, int i0, i
     const int kind = (int)(rest % kinds);
     const int b = (int)((rest / kinds) % a.B);
     const int i = i0 + (int)((rest / kinds) / a.B);
-    const int drafts = drafts_of(a, b);
-    if (i + kind > drafts) continue;                 // uniform: not a row of this sequence
-    const int64_t at = (int64_t)i * a.B + b;
+    if (i + kind > drafts_of(a, b)) continue;        // uniform: not a row of this sequence
     const Tin* z = kind ? draft_row<Tin>(a, b, i) : target_row<Tin>(a, b, i);
     const RowSplit sp = split_row(z, a.V);
     const int c0 = (int)((int64_t)sp.nfull * part / a.parts);
     const int n = (int)((int64_t)sp.nfull * (part + 1) / a.parts) - c0;
     const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + sp.lead + (int64_t)c0 * E, n * 16);
-    u32x4 r[U];
+    uint32_t r[U][4];
 #pragma unroll
-    for (int u = 0; u < U; ++u) r[u] = buf_load16<kAuxLast>(rz, u * NT + tid < n ? (u * NT + tid) * 16 : kOff, 0);
+    for (int u = 0; u < U; ++u) load16<kAuxLast>(r[u], rz, tid * 16, u * NT * 16);
     if (i0 > 0) {
       __syncthreads();                               // the last item's flag is read
       if (tid < 64) {
-        const bool on = decide<Tin>(a, b, i0, false).mode == kDrawTarget;
-        if (tid == 0) alive = on;
+        const int s = first_stop<Tin>(a, b, 0, i0, false).status;
+        if (tid == 0) alive = s == kAccept || s == kUnclear;
       }
       __syncthreads();
       if (!alive) continue;
     }
-    float m = -INFINITY;                             // this thread's maximum
-    double s = 0.0, ref = 0.0;                       // ref: m, or 0 while that is -inf
-    auto add = [&](const auto& x, float cm) {
-      if (cm > m) {
-        s *= exp2_f64(((double)m - (double)cm) * a.t2e);
-        m = cm;
-        ref = cm;
-      }
-      // the difference first: a product with a far logit (a mask of the type's lowest value) has no
-      // fraction left
+    float N = -INFINITY, m = -INFINITY;              // 2^N s so far; the largest logit
+    double s = 0.0;
+    auto add = [&](const auto& x) {
+      const float cm = max_of(x);
+      const float nc = __builtin_ceilf(cm * L);
+      const float sh = (nc == -INFINITY) ? 0.0f : nc;
+      float e[sizeof(x) / 4];
 #pragma unroll
-      for (int j = 0; j < (int)(sizeof(x) / 4); ++j) s += exp2_f64(((double)x[j] - ref) * a.t2e);
+      for (int j = 0; j < (int)(sizeof(x) / 4); ++j) e[j] = exp2_hw(__builtin_fmaf(x[j], L, -sh));
+      float cs = e[0];
+      if constexpr (sizeof(x) == 32) cs = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+      if constexpr (sizeof(x) == 16) cs = (e[0] + e[1]) + (e[2] + e[3]);
+      // integer shifts: the scales are exact
+      const float M = fmaxf(N, nc);
+      const float fa = (N == M) ? 1.0f : exp2_hw(N - M);
+      const float fb = (nc == M) ? 1.0f : exp2_hw(nc - M);
+      s = s * (double)fa + (double)(cs * fb);
+      N = M;
+      m = fmaxf(m, cm);
     };
     if (part == 0 && tid < sp.nedge) {
-      const float x[1] = {entry_value(z, sp.entry<E>(tid))};
-      add(x, x[0]);
+      const float x[1] = {entry_value(z, sp.template entry<E>(tid))};
+      add(x);
     }
     for (int base = 0; base < n; base += U * NT) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int c = base + u * NT + tid;
+        if (base + u * NT >= n) break;               // uniform
         float x[E];
         unpack<Tin>(r[u], x);
-        r[u] = buf_load16<kAuxLast>(rz, c + U * NT < n ? (c + U * NT) * 16 : kOff, 0);
-        if (c < n) {
-          float cm = max3(x[0], x[1], x[2]);
-          if constexpr (E == 8) cm = max3(cm, max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
-          else cm = fmaxf(cm, x[3]);
-          add(x, cm);
-        }
+        if (base + (U + u) * NT < n) load16<kAuxLast>(r[u], rz, tid * 16, (base + (U + u) * NT) * 16);
+        if (tid < n - base - u * NT) add(x);
       }
     }
-    double md = m;
-    {
-      // the wave's maximum, then one exponential per thread (NaN sums stay NaN)
-      const double M = wave_max_f64(md);
-      s = wave_sum_f64(md == M ? s : s * exp2_f64((md - M) * a.t2e));
-      md = M;
-    }
+    // the wave's largest shift, then one exact scale per thread
+    const float M = wave_max(N);
+    s = wave_sum_f64(N == M ? s : s * (double)exp2_hw(N - M));
+    m = wave_max(m);
     __syncthreads();                                 // the last item's partials are read
     if ((tid & 63) == 0) {
-      red[tid >> 6] = md;
+      red[tid >> 6] = M;
       red[NW + (tid >> 6)] = s;
+      red[2 * NW + (tid >> 6)] = m;
     }
     __syncthreads();
     if (tid == 0) {
-      for (int w = 1; w < NW; ++w) join(md, s, red[w], red[NW + w], a.t2e);
-      double* out = a.stats + ((at * 2 + kind) * a.parts + part) * 2;
-      out[0] = md;
-      out[1] = s;
+      VerifyPart o = {red[0], 0.0, red[2 * NW]};
+      for (int w = 1; w < NW; ++w) {
+        o.n = fmax(o.n, red[w]);
+        o.m = fmax(o.m, red[2 * NW + w]);
+      }
+      for (int w = 0; w < NW; ++w) o.s += red[w] == o.n ? red[NW + w] : red[NW + w] * exp2_f64(red[w] - o.n);
+      a.stats[(((int64_t)i * a.B + b) * 2 + kind) * a.parts + part] = o;
     }
   }
 }
 
-// Weights of the E entries from entry e0 on (a whole chunk of the target's row).
-template <typename Tin>
-__device__ __forceinline__ void chunk_weights(const VerifyArgs& a, const VerifyDraw& d, int mode, const Tin* p,
-                                              const Tin* q, int x, int e0, double (&w)[16 / sizeof(Tin)]) {
-  constexpr int E = 16 / (int)sizeof(Tin);
-  float z[E];
-  unpack<Tin>(*(const u32x4*)(p + e0), z);
-#pragma unroll
-  for (int j = 0; j < E; ++j) w[j] = exp2_f64(log2_prob(a, d.p, z[j]));
-  if (mode == kDrawResidual) {
-    if (((uintptr_t)(q + e0) & 15) == 0) {
-      unpack<Tin>(*(const u32x4*)(q + e0), z);
-    } else {
-#pragma unroll
-      for (int j = 0; j < E; ++j) z[j] = entry_value(q, e0 + j);
-    }
-#pragma unroll
-    for (int j = 0; j < E; ++j) w[j] = fmax(w[j] - exp2_f64(log2_prob(a, d.q, z[j])), 0.0);
-  } else if (mode == kDrawWithout) {
-#pragma unroll
-    for (int j = 0; j < E; ++j) w[j] = e0 + j == x ? 0.0 : w[j];
-  }
-}
-template <typename Tin>
-__device__ __forceinline__ double entry_weight(const VerifyArgs& a, const VerifyDraw& d, int mode, const Tin* p,
-                                               const Tin* q, int x, int e) {
-  double w = exp2_f64(log2_prob(a, d.p, entry_value(p, e)));
-  if (mode == kDrawResidual) w = fmax(w - exp2_f64(log2_prob(a, d.q, entry_value(q, e))), 0.0);
-  else if (mode == kDrawWithout && e == x)
-    w = 0.0;
-  return w;
+// ------------------------------------------------------------------ exact rows (rare)
+// log2 of an entry's probability under an exact normaliser.
+__device__ __forceinline__ double log2_prob(const VerifyArgs& a, const VerifyNorm& n, float z) {
+  return __builtin_fma((double)z - n.m, a.t2e, -n.log2s);
 }
 
-// Cell 0 holds the entries before the row's whole chunks, cell c the 64 chunks from 64 (c - 1) on, the
-// last cell the entries behind them. A lane's entries of a cell: `count` of them from `first` on.
+// A row's exact normaliser, by the workgroup; log2s is NaN for a row holding NaN or +inf, or only -inf.
+template <typename Tin, int NT>
+__device__ VerifyNorm exact_norm(const VerifyArgs& a, const Tin* z, double* red) {
+  constexpr int NW = NT / 64;
+  float m = -INFINITY;
+  for (int e = threadIdx.x; e < a.V; e += NT) m = fmaxf(m, entry_value(z, e));
+  m = wave_max(m);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  double M = red[0];
+  for (int w = 1; w < NW; ++w) M = fmax(M, red[w]);
+  double s = 0.0;
+  if (M != -INFINITY)
+    for (int e = threadIdx.x; e < a.V; e += NT) s += exp2_f64(((double)entry_value(z, e) - M) * a.t2e);
+  s = wave_sum_f64(s);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int w = 0; w < NW; ++w) s += red[w];
+  __syncthreads();
+  return {M, s > 0.0 && s < INFINITY ? log2_f64(s) : (double)__builtin_nanf("")};
+}
+
+// ------------------------------------------------------------------ weights
+// p and q of E logits each, as scaled (VerifyDraw); entries below 2^-1000 of p's or q's scale are
+// held there, and flushed where that could show.
+constexpr double kFlush = 1e-280;
+__device__ __forceinline__ float lowest_logit(const VerifyArgs& a, double s) {
+  return (float)((-s / kExpTable - 1000.0) / a.t2e);
+}
+template <int E>
+__device__ __forceinline__ void probs(const VerifyArgs& a, const VerifyDraw& d, double s, const VerifyNorm& n,
+                                      const float (&z)[E], const double* table, double (&w)[E]) {
+  if (d.far) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) w[j] = exp2_f64(log2_prob(a, n, z[j]));
+  } else {
+    const double K = a.t2e * kExpTable, sm = s + kRoundMagic;
+    const float low = lowest_logit(a, s);
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+      w[j] = exp2_tab((double)__builtin_elementwise_maximum(z[j], low), K, sm, table);
+  }
+}
+
+// Cell 0 holds the entries before the target row's whole chunks, cell c the 64 chunks from 64 (c - 1)
+// on, the last cell the entries behind them. A lane's entries of a cell: `count` of them (a chunk or a
+// single one) from `first` on.
 struct CellSpan {
   int first, count;
 };
@@ -272,78 +315,173 @@ __device__ __forceinline__ CellSpan cell_span(const RowSplit& sp, int V, int cel
   const int c = (cell - 1) * 64 + lane;
   return {sp.lead + c * E, c < sp.nfull ? E : 0};
 }
+// Its logits in `row`, -inf past the span. chunks: the span's start is 16-byte aligned in this row.
 template <typename Tin>
-__device__ __forceinline__ void span_weights(const VerifyArgs& a, const VerifyDraw& d, int mode, const Tin* p,
-                                             const Tin* q, int x, const CellSpan& s, double (&w)[16 / sizeof(Tin)]) {
+__device__ __forceinline__ void span_logits(const Tin* row, const CellSpan& s, bool chunks, float (&z)[16 / sizeof(Tin)]) {
   constexpr int E = 16 / (int)sizeof(Tin);
-  if (s.count == E) {
-    chunk_weights(a, d, mode, p, q, x, s.first, w);
+  if (s.count == E && chunks) {
+    unpack<Tin>(*(const u32x4*)(row + s.first), z);
   } else {
 #pragma unroll
-    for (int j = 0; j < E; ++j) w[j] = 0.0;
-    if (s.count == 1) w[0] = entry_weight(a, d, mode, p, q, x, s.first);
+    for (int j = 0; j < E; ++j) z[j] = j < s.count ? entry_value(row, s.first + j) : -INFINITY;
   }
 }
 
-// The sum of a cell's weights, by one wave.
+// A row drawn from, and the workgroup's handle on it.
 template <typename Tin>
-__device__ __forceinline__ double cell_sum(const VerifyArgs& a, const VerifyDraw& d, int mode, const Tin* p,
-                                           const Tin* q, int x, const RowSplit& sp, int cell) {
-  constexpr int E = 16 / (int)sizeof(Tin);
-  double w[E];
-  span_weights(a, d, mode, p, q, x, cell_span<Tin>(sp, a.V, a.cells, cell, threadIdx.x & 63), w);
-  double s = 0.0;
-#pragma unroll
-  for (int j = 0; j < E; ++j) s += w[j];
-  return wave_sum_f64(s);
+struct DrawRows {
+  const Tin *p, *q;
+  bool q_chunks;         // q's rows have p's offset within 16 bytes
+  int x;                 // the drafted token that p is drawn without, or -1
+  RowSplit split;
+};
+template <typename Tin>
+__device__ __forceinline__ DrawRows<Tin> draw_rows(const VerifyArgs& a, const VerifyDraw& d, int64_t b) {
+  DrawRows<Tin> r;
+  r.p = target_row<Tin>(a, b, d.pos);
+  r.q = d.mode == kDrawResidual ? draft_row<Tin>(a, b, d.pos) : nullptr;
+  r.q_chunks = (((uintptr_t)r.p - (uintptr_t)r.q) & 15) == 0;
+  r.x = d.mode == kDrawWithout ? (int)a.ids[b * a.D + d.pos] : -1;
+  r.split = split_row(r.p, a.V);
+  return r;
 }
 
+// ------------------------------------------------------------------ cells
 template <typename Tin>
 __global__ __launch_bounds__(kCellNT) void verify_cells(VerifyArgs a) {
-  __shared__ VerifyDraw ds;
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  constexpr int E = 16 / (int)sizeof(Tin);
+  constexpr int NW = kCellNT / 64;
+  __shared__ double table[kExpTable];
+  __shared__ double red[NW];
+  __shared__ Stop stop_s;
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  exp2_table_fill(table);
   for (int64_t item = blockIdx.x; item < (int64_t)a.B * a.draw_parts; item += gridDim.x) {
     const int b = (int)(item / a.draw_parts);
     const int part = (int)(item % a.draw_parts);
-    __syncthreads();
-    if (wave == 0) {
-      const int n = drafts_of(a, b);
-      VerifyDraw d = decide<Tin>(a, b, n, part == 0);
-      if (d.mode == kDrawTarget) {
-        d.p = row_norm(a, b, n, 0);
-        if (d.p.log2s != d.p.log2s) d.mode = kDrawBad;
+    const int n = drafts_of(a, b);
+    // where the sequence stops; every workgroup of a sequence comes to the same answer
+    VerifyDraw d{};
+    for (int from = 0;;) {
+      __syncthreads();                               // the table is written, stop_s is read
+      if (wave == 0) {
+        const Stop s = first_stop<Tin>(a, b, from, n, part == 0);
+        if (tid == 0) stop_s = s;
       }
-      if (threadIdx.x == 0) {
-        ds = d;
-        if (part == 0) a.draw[b] = d;
+      __syncthreads();
+      const Stop s = stop_s;
+      d.pos = s.pos;
+      d.mode = s.status == kBadRow ? kDrawBad
+               : s.pos == n        ? kDrawTarget
+                                   : (a.draft ? kDrawResidual : kDrawWithout);
+      if (s.status != kUnclear) break;
+      // within the statistics' error, or beyond their range: from exact sums over the two rows
+      const int64_t x = a.ids[(int64_t)b * a.D + s.pos];
+      const Tin* p = target_row<Tin>(a, b, s.pos);
+      d.p = exact_norm<Tin, kCellNT>(a, p, red);
+      d.q = {0.0, 0.0};
+      double q = 1.0;
+      if (a.draft) {
+        const Tin* qr = draft_row<Tin>(a, b, s.pos);
+        d.q = exact_norm<Tin, kCellNT>(a, qr, red);
+        q = exp2_f64(log2_prob(a, d.q, entry_value(qr, x)));
       }
+      const double lp = log2_prob(a, d.p, entry_value(p, x));
+      if (d.p.log2s != d.p.log2s || d.q.log2s != d.q.log2s) {
+        d.mode = kDrawBad;
+        break;
+      }
+      if (!((double)a.u[(int64_t)b * a.D + s.pos] * q < exp2_f64(lp))) break;
+      if (part == 0 && tid == 0) {
+        a.tokens[(int64_t)b * (a.D + 1) + s.pos] = x;
+        a.logp[(int64_t)b * (a.D + 1) + s.pos] = (float)(lp * kLn2F64);
+      }
+      from = s.pos + 1;
     }
-    __syncthreads();
-    const VerifyDraw d = ds;
-    if (d.mode == kDrawBad) continue;
-    const Tin* p = target_row<Tin>(a, b, d.pos);
-    const Tin* q = d.mode == kDrawResidual ? draft_row<Tin>(a, b, d.pos) : nullptr;
-    const int x = d.mode == kDrawWithout ? (int)a.ids[(int64_t)b * a.D + d.pos] : -1;
-    const RowSplit sp = split_row(p, a.V);
+    if (d.mode != kDrawBad) {
+      const RowNorm p = row_norm(a, b, d.pos, 0);
+      RowNorm q{};
+      if (d.mode == kDrawResidual) q = row_norm(a, b, d.pos, 1);
+      d.far = p.far || q.far;
+      if (p.bad || q.bad) d.mode = kDrawBad;
+      if (d.far && d.mode != kDrawBad) {             // uniform
+        d.p = exact_norm<Tin, kCellNT>(a, target_row<Tin>(a, b, d.pos), red);
+        if (d.mode == kDrawResidual) d.q = exact_norm<Tin, kCellNT>(a, draft_row<Tin>(a, b, d.pos), red);
+        else d.q = {0.0, 0.0};
+        if (d.p.log2s != d.p.log2s || d.q.log2s != d.q.log2s) d.mode = kDrawBad;
+      }
+      d.sp = -__builtin_rint(p.lse2 * kExpTable);
+      d.sq = -__builtin_rint(q.lse2 * kExpTable);
+      d.phi = d.far ? 1.0
+                    : exp2_f64(((-d.sq / kExpTable) - q.lse2) - ((-d.sp / kExpTable) - p.lse2));
+    }
+    if (part == 0 && tid == 0) a.draw[b] = d;
+    if (d.mode == kDrawBad) continue;                // uniform
+    const DrawRows<Tin> rows = draw_rows<Tin>(a, d, b);
     const int w0 = (int)((int64_t)a.cells * part / a.draw_parts);
     const int w1 = (int)((int64_t)a.cells * (part + 1) / a.draw_parts);
-    for (int cell = w0 + wave; cell < w1; cell += kCellNT / 64) {
-      const double s = cell_sum(a, d, d.mode, p, q, x, sp, cell);
-      if ((threadIdx.x & 63) == 0) a.cell[(int64_t)b * a.cells + cell] = s;
+    // the next cell's logits are read ahead
+    float zp[E], zq[E];
+    auto fetch = [&](int cell) {
+      const CellSpan s = cell < w1 ? cell_span<Tin>(rows.split, a.V, a.cells, cell, lane) : CellSpan{0, 0};
+      span_logits(rows.p, s, true, zp);
+      if (d.mode == kDrawResidual) span_logits(rows.q, s, rows.q_chunks, zq);
+      return s;
+    };
+    CellSpan s = fetch(w0 + wave);
+    for (int cell = w0 + wave; cell < w1; cell += NW) {
+      const CellSpan now = s;
+      float cp[E], cq[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        cp[j] = zp[j];
+        cq[j] = zq[j];
+      }
+      s = fetch(cell + NW);
+      VerifyCell c = {0.0, 0.0, 0.0, 0.0};
+      double w[E];
+      probs(a, d, d.sp, d.p, cp, table, w);
+#pragma unroll
+      for (int j = 0; j < E; ++j) c.p += w[j];
+      if (d.mode == kDrawResidual) {
+        double v[E];
+        probs(a, d, d.sq, d.q, cq, table, v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          c.q += v[j];
+          const double r = __builtin_fma(-d.phi, v[j], w[j]);
+          c.r += r > 0.0 ? r : 0.0;
+          c.slope += r > 0.0 ? v[j] : 0.0;
+        }
+        c.q = wave_sum_f64(c.q);
+        c.slope = wave_sum_f64(c.slope);
+      } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) c.r += now.first + j == rows.x ? 0.0 : w[j];
+      }
+      c.r = wave_sum_f64(c.r > kFlush ? c.r : 0.0);
+      c.p = wave_sum_f64(c.p > kFlush ? c.p : 0.0);
+      if (lane == 0) a.cell[(int64_t)b * a.cells + cell] = c;
     }
   }
 }
 
+// ------------------------------------------------------------------ the draw
 template <typename Tin>
 __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int NT = kPickNT;
   constexpr int NW = NT / 64;
-  __shared__ double wsum[2][NW];
+  __shared__ double table[kExpTable];
+  __shared__ double wsum[3][NW];
   __shared__ double before_s;
   __shared__ int found_s, last_s;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
+  const int wave = tid >> 6;
+  exp2_table_fill(table);
   for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
     const VerifyDraw d = a.draw[b];
     int64_t* tokens = a.tokens + b * (a.D + 1);
@@ -360,44 +498,62 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
       }
       continue;
     }
-    const Tin* p = target_row<Tin>(a, b, d.pos);
-    const Tin* q = d.mode == kDrawResidual ? draft_row<Tin>(a, b, d.pos) : nullptr;
-    const int x = d.mode == kDrawWithout ? (int)a.ids[b * a.D + d.pos] : -1;
-    const RowSplit sp = split_row(p, a.V);
-    double* cell = a.cell + b * a.cells;
-    int mode = d.mode;
-    const int run = (a.cells + NT - 1) / NT;          // cells per thread, consecutive
+    const VerifyCell* cell = a.cell + b * a.cells;
+    const int run = (a.cells + NT - 1) / NT;         // cells per thread, consecutive
     const int r0 = min(tid * run, a.cells), r1 = min(r0 + run, a.cells);
-    double before = 0.0, total = 0.0;                // the cells before this thread's, and all of them
-    for (int attempt = 0; attempt < 2; ++attempt) {
-      double own = 0.0;
-      for (int c = r0; c < r1; ++c) own += cell[c];
+    // p's and q's exact totals: the scale that q has to have against p
+    double tp = 0.0, tq = 0.0;
+    for (int c = r0; c < r1; ++c) {
+      tp += cell[c].p;
+      tq += cell[c].q;
+    }
+    tp = wave_sum_f64(tp);
+    tq = wave_sum_f64(tq);
+    if (lane == 0) {
+      wsum[0][wave] = tp;
+      wsum[1][wave] = tq;
+    }
+    if (tid == 0) {
+      found_s = a.cells;
+      last_s = -1;
+    }
+    __syncthreads();
+    tp = tq = 0.0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      tp += wsum[0][w];
+      tq += wsum[1][w];
+    }
+    bool residual = d.mode == kDrawResidual;
+    const double scale = residual ? tp / tq : 0.0;   // of q; phi is the scale the cells used
+    bool from_p = d.mode == kDrawTarget;
+    auto weight = [&](int c) {
+      if (from_p) return cell[c].p;
+      const double r = cell[c].r - (scale - d.phi) * cell[c].slope;
+      return residual ? fmax(r, 0.0) : r;
+    };
+    double before = 0.0, total = 0.0, own = 0.0;     // the cells before this thread's, all, its own
+    for (;;) {
+      own = 0.0;
+      for (int c = r0; c < r1; ++c) own += weight(c);
       double incl = own;
 #pragma unroll
       for (int off = 1; off < 64; off <<= 1) {
         const double o = __shfl_up(incl, off, 64);
         if (lane >= off) incl += o;
       }
-      if (lane == 63) wsum[attempt][tid >> 6] = incl;
-      if (tid == 0) {
-        found_s = a.cells;
-        last_s = -1;
-      }
+      if (lane == 63) wsum[2][wave] = incl;
       __syncthreads();
       total = 0.0;
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
-        if (w == tid >> 6) before = total + (incl - own);
-        total += wsum[attempt][w];
+        if (w == wave) before = total + (incl - own);
+        total += wsum[2][w];
       }
-      if (total > 0.0) break;                        // uniform
-      // p - q has no positive part: the draw is from p (the sums again, in this workgroup)
-      mode = kDrawTarget;
-      for (int c = tid >> 6; c < a.cells; c += NW) {
-        const double s = cell_sum(a, d, mode, p, q, x, sp, c);
-        if (lane == 0) cell[c] = s;
-      }
-      __threadfence_block();
+      // p - q without a positive part beyond rounding (p = q): the draw is from p
+      if (from_p || total > 1e-12 * tp) break;       // uniform
+      from_p = true;
+      residual = false;
       __syncthreads();
     }
     const double goal = (double)a.u_new[b] * total;
@@ -406,7 +562,7 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
     {
       double c = before;
       for (int i = r0; i < r1; ++i) {
-        const double w = cell[i];
+        const double w = weight(i);
         if (w > 0.0) atomicMax(&last_s, i);
         if (c + w > goal && w > 0.0) {
           atomicMin(&found_s, i);
@@ -419,24 +575,37 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
     }
     __syncthreads();
     const int found = found_s < a.cells ? found_s : last_s;   // total > 0: some weight is positive
-    if (hit_cell == found) before_s = hit_before;             // one thread, if a cell was hit
+    if (hit_cell == found) before_s = hit_before;
     __syncthreads();
     if (tid < 64 && found >= 0) {
-      double c = before_s;                                    // no cell hit: not used, c > goal fails
-      if (found_s == a.cells) c = -INFINITY;
-      const CellSpan s = cell_span<Tin>(sp, a.V, a.cells, found, lane);
+      const DrawRows<Tin> rows = draw_rows<Tin>(a, d, b);
+      const CellSpan s = cell_span<Tin>(rows.split, a.V, a.cells, found, lane);
+      float z[E];
       double w[E];
-      span_weights(a, d, mode, p, q, x, s, w);
+      span_logits(rows.p, s, true, z);
+      probs(a, d, d.sp, d.p, z, table, w);
+      if (residual) {
+        double v[E];
+        float y[E];
+        span_logits(rows.q, s, rows.q_chunks, y);
+        probs(a, d, d.sq, d.q, y, table, v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) w[j] = __builtin_fma(-scale, v[j], w[j]);
+      }
       double mine = 0.0;
 #pragma unroll
-      for (int j = 0; j < E; ++j) mine += w[j];
+      for (int j = 0; j < E; ++j) {
+        if (!(w[j] > kFlush) || (!from_p && s.first + j == rows.x)) w[j] = 0.0;
+        mine += w[j];
+      }
       double incl = mine;
 #pragma unroll
       for (int off = 1; off < 64; off <<= 1) {
         const double o = __shfl_up(incl, off, 64);
         if (lane >= off) incl += o;
       }
-      c += incl - mine;
+      // no cell passed the goal (rounding, or u = 1): the last positive weight
+      double c = (found_s < a.cells ? before_s : -INFINITY) + (incl - mine);
       int hit = -1, last = -1;
 #pragma unroll
       for (int j = 0; j < E; ++j) {
@@ -453,8 +622,14 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
       else if (lasts) v = __shfl(last, 63 - __builtin_clzll(lasts), 64);
       if (lane == 0) {
         tokens[d.pos] = v;
-        logp[d.pos] = v >= 0 ? (float)(log2_prob(a, d.p, entry_value(p, v)) * kLn2F64)
-                             : __builtin_nanf("");
+        float out = __builtin_nanf("");
+        if (v >= 0) {
+          const float zv = entry_value(rows.p, v);
+          const double l = d.far ? log2_prob(a, d.p, zv)
+                                 : __builtin_fma((double)zv, a.t2e, d.sp / kExpTable) - log2_f64(tp);
+          out = (float)(l * kLn2F64);
+        }
+        logp[d.pos] = out;
       }
     }
     __syncthreads();                                 // the sequence's LDS is read
@@ -478,15 +653,13 @@ int64_t verify_layout(VerifyArgs& a, int es, bool with_draft, void* workspace) {
     o += (bytes + 15) & ~(int64_t)15;
     return p;
   };
-  a.stats = (double*)take((int64_t)(a.D + 1) * a.B * 2 * a.parts * 16);
-  a.cell = (double*)take((int64_t)a.B * a.cells * 8);
+  a.stats = (VerifyPart*)take((int64_t)(a.D + 1) * a.B * 2 * a.parts * sizeof(VerifyPart));
+  a.cell = (VerifyCell*)take((int64_t)a.B * a.cells * sizeof(VerifyCell));
   a.draw = (VerifyDraw*)take((int64_t)a.B * sizeof(VerifyDraw));
   return o;
 }
 
 hipError_t launch_verify(const VerifyArgs& a, bool bf16, hipStream_t st) {
-  const unsigned g2 = (unsigned)std::min<int64_t>((int64_t)a.B * a.draw_parts, kLaunchThreads / kCellNT);
-  const unsigned g3 = (unsigned)std::min<int64_t>(a.B, kLaunchThreads / kPickNT);
   // Positions in groups that fill the device; a sequence that an earlier group stops is not read on.
   // At most eight launches however many drafts there are.
   const int64_t per = (int64_t)a.B * (a.draft ? 2 : 1);
@@ -497,6 +670,8 @@ hipError_t launch_verify(const VerifyArgs& a, bool bf16, hipStream_t st) {
     if (bf16) verify_stats<uint16_t><<<g1, kStatsNT, 0, st>>>(a, i0, i1);
     else verify_stats<float><<<g1, kStatsNT, 0, st>>>(a, i0, i1);
   }
+  const unsigned g2 = (unsigned)std::min<int64_t>((int64_t)a.B * a.draw_parts, kLaunchThreads / kCellNT);
+  const unsigned g3 = (unsigned)std::min<int64_t>(a.B, kLaunchThreads / kPickNT);
   if (bf16) {
     verify_cells<uint16_t><<<g2, kCellNT, 0, st>>>(a);
     verify_pick<uint16_t><<<g3, kPickNT, 0, st>>>(a);

@@ -12,7 +12,8 @@ Tolerances, from the kernels' arithmetic (u: half a rounding step of a type, 2^-
     exponential of z L - lse2, |z L - lse2| <= 150 in the tests: 150 * 2^-24 * ln 2 = 6.2e-6, and
     the log-sum-exp's 4.1e-6); results below the type's normal range are flushed or rounded by up
     to 2^-126.
-  * log-probs of verify_drafts: 64 bits rounded once: u |lp|, and 1e-11 for the 64-bit sums.
+  * log-probs of verify_drafts: of accepted drafts, rounded once (u |lp|) from a row's log-sum-exp as
+    above (LSE); of the drawn token, rounded once from 64-bit sums (1e-11).
 """
 import numpy as np
 import torch

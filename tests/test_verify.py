@@ -5,7 +5,7 @@ import torch
 
 import oracle
 import paper_2605_12070_amd as P
-from operator_helpers import DEV, near, rows, values_of
+from operator_helpers import DEV, LSE, near, values_of
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -33,7 +33,9 @@ def check(z, ids, u, un, q=None, n=None, tau=1.0):
                                         None if n is None else n.cpu().numpy(), tau)
     assert np.array_equal(r.accepted.cpu().numpy(), acc), "accepted"
     assert np.array_equal(r.tokens.cpu().numpy(), tok), "tokens"
-    near(r.logp.cpu().numpy(), lp, 2.0 ** -24 * np.abs(np.nan_to_num(lp)) + 1e-11, "logp")
+    drawn = np.arange(D1)[None] == acc[:, None]
+    tol = np.where(drawn, 1e-11, LSE) + 2.0 ** -24 * np.abs(np.nan_to_num(lp))
+    near(r.logp.cpu().numpy(), lp, tol, "logp")
     return r
 
 
