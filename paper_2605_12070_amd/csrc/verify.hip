@@ -29,7 +29,7 @@ namespace {
 
 constexpr int kStatsNT = 256;
 constexpr int kCellNT = 256;
-constexpr int kPickNT = 256;
+constexpr int kPickNT = 512;
 constexpr int kMaxParts = 16;
 constexpr int64_t kStatsRows = 512;   // rows of a launch of the statistics
 
@@ -80,73 +80,105 @@ struct RowNorm {
   double lse2, err;
   bool far, bad;
 };
-__device__ __forceinline__ RowNorm row_norm(const VerifyArgs& a, int64_t b, int64_t i, int kind) {
-  const VerifyPart* st = a.stats + ((i * a.B + b) * 2 + kind) * a.parts;
-  double n = -INFINITY, m = -INFINITY;
-  for (int p = 0; p < a.parts; ++p) {
-    n = fmax(n, st[p].n);
-    m = fmax(m, st[p].m);
+enum Status { kAccept, kReject, kUnclear, kBadRow };
+struct Stop {
+  int pos, status;
+};
+
+// A window of a sequence's positions, for the workgroup that looks through it.
+constexpr int kWindow = 16;
+struct StopState {
+  RowNorm norm[2][kWindow + 1];   // of the target's and the draft's rows from position `from` on
+  int from;
+  Stop stop;
+};
+
+// The parts of the window's rows joined: a group of lanes per row, so that their loads are in flight
+// together. Called by the whole workgroup (NT threads), barriers around it are the caller's.
+template <int NT>
+__device__ __forceinline__ void window_norms(const VerifyArgs& a, int64_t b, int from, int n, StopState& st) {
+  const int lanes = a.parts > 8 ? 16 : a.parts > 4 ? 8 : a.parts > 2 ? 4 : a.parts;
+  const int part = (int)threadIdx.x % lanes;
+  const int rows = min(kWindow, n - from) + 1;       // of the target; the draft has none behind the last
+  for (int row = (int)threadIdx.x / lanes; row < 2 * (kWindow + 1); row += NT / lanes) {
+    const int kind = row & 1, i = row >> 1;
+    const bool in = i < rows && (kind == 0 || (a.draft && from + i < n));
+    VerifyPart v = {-INFINITY, 0.0, -INFINITY};
+    if (in && part < a.parts) v = a.stats[(((int64_t)(from + i) * a.B + b) * 2 + kind) * a.parts + part];
+    double N = v.n, m = v.m;
+    for (int off = 1; off < lanes; off <<= 1) {
+      N = fmax(N, __shfl_xor(N, off, 64));
+      m = fmax(m, __shfl_xor(m, off, 64));
+    }
+    double s = v.n == -INFINITY ? 0.0 : v.s * exp2_f64(v.n - N);
+    for (int off = 1; off < lanes; off <<= 1) s += __shfl_xor(s, off, 64);
+    if (!in || part != 0) continue;
+    RowNorm r;
+    r.far = !(fabs(m) * a.t2e < 1048576.0);
+    r.bad = !r.far && !(s > 0.0 && s < INFINITY);
+    r.lse2 = r.far || r.bad ? 0.0 : N + log2_f64(s);
+    // Terms: the exponential (2^-22) and a chunk's additions (2^-22); its argument's rounding, 2^-24 of
+    // log2 units below the maximum, which weighs at most log2(V) <= 28 over the row; the 32-bit log2(e)
+    // / temperature, 2^-25 of the logits that matter. In all below 2.7e-6 + |m t2e| 2^-24 of the sum.
+    r.err = 8e-6 + fabs(r.lse2) * 2.4e-7;
+    st.norm[kind][i] = r;
   }
-  double s = 0.0;
-  for (int p = 0; p < a.parts; ++p)
-    if (st[p].n != -INFINITY) s += st[p].s * exp2_f64(st[p].n - n);
-  RowNorm r;
-  r.far = !(fabs(m) * a.t2e < 1048576.0);
-  r.bad = !r.far && !(s > 0.0 && s < INFINITY);
-  r.lse2 = r.far || r.bad ? 0.0 : n + log2_f64(s);
-  // Terms: the exponential (2^-22) and a chunk's additions (2^-22); its argument's rounding, 2^-24 of
-  // log2 units below the maximum, which weighs at most log2(V) <= 28 over the row; the 32-bit log2(e) /
-  // temperature, 2^-25 of the logits that matter. In all below 2.7e-6 + |m t2e| 2^-24 of the sum.
-  r.err = 8e-6 + fabs(r.lse2) * 2.4e-7;
-  return r;
 }
 
-enum Status { kAccept, kReject, kUnclear, kBadRow };
-
-// The first of the drafts [i0, n) of sequence b that is not clearly accepted, by one wave: every lane
-// returns the same position (n if there is none) and its status. With `write`, the accepted drafts
-// and their log-probs go to the outputs. (Lanes behind that draft may read statistics that were
-// never computed; they decide nothing.)
-struct Stop {
-  int pos;
-  int status;
-};
-template <typename Tin>
-__device__ __forceinline__ Stop first_stop(const VerifyArgs& a, int b, int i0, int n, bool write) {
-  const int lane = threadIdx.x & 63;
-  for (; i0 < n; i0 += 64) {
-    const int i = i0 + lane;
-    int status = kAccept;
-    float out = 0.0f;
-    int64_t x = -1;
-    if (i < n) {
-      x = a.ids[(int64_t)b * a.D + i];
-      const RowNorm p = row_norm(a, b, i, 0);
-      RowNorm q{};
-      if (a.draft) q = row_norm(a, b, i, 1);
-      if (x < 0 || x >= a.V || p.bad || q.bad) {
-        status = kBadRow;
-      } else if (p.far || q.far) {
-        status = kUnclear;
-      } else {
-        const double lp = __builtin_fma((double)entry_value(target_row<Tin>(a, b, i), x), a.t2e, -p.lse2);
-        const double lq = a.draft ? __builtin_fma((double)entry_value(draft_row<Tin>(a, b, i), x), a.t2e, -q.lse2) : 0.0;
-        const double uq = (double)a.u[(int64_t)b * a.D + i] * exp2_f64(lq), pp = exp2_f64(lp);
-        const double mu = p.err + q.err;
-        status = uq * (1.0 + mu) < pp ? kAccept : (uq < pp * (1.0 + mu) ? kUnclear : kReject);
-        if (pp == 0.0) status = kReject;
-        out = (float)(lp * kLn2F64);
+// The first of the drafts [from, n) of sequence b that is not clearly accepted (position n if there is
+// none) and its status, by the whole workgroup. With `write`, the accepted drafts and their log-probs
+// go to the outputs. Rows behind that draft may have statistics that were never computed; they decide
+// nothing. Afterwards st.norm holds the position's rows, at st.stop.pos - st.from.
+template <typename Tin, int NT>
+__device__ __forceinline__ Stop first_stop(const VerifyArgs& a, int b, int from, int n, bool write, StopState& st) {
+  for (;; from += kWindow) {
+    __syncthreads();                                 // st is read
+    window_norms<NT>(a, b, from, n, st);
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      const int lane = threadIdx.x;
+      const int i = from + lane;
+      const bool in = lane < kWindow && i < n;
+      int status = kAccept;
+      float out = 0.0f;
+      int64_t x = -1;
+      if (in) {
+        x = a.ids[(int64_t)b * a.D + i];
+        const RowNorm p = st.norm[0][lane];
+        RowNorm q{};
+        if (a.draft) q = st.norm[1][lane];
+        if (x < 0 || x >= a.V || p.bad || q.bad) {
+          status = kBadRow;
+        } else if (p.far || q.far) {
+          status = kUnclear;
+        } else {
+          const float zp = entry_value(target_row<Tin>(a, b, i), x);
+          const float zq = a.draft ? entry_value(draft_row<Tin>(a, b, i), x) : 0.0f;
+          const double lp = __builtin_fma((double)zp, a.t2e, -p.lse2);
+          const double q_x = a.draft ? exp2_f64(__builtin_fma((double)zq, a.t2e, -q.lse2)) : 1.0;
+          const double uq = (double)a.u[(int64_t)b * a.D + i] * q_x, pp = exp2_f64(lp);
+          const double mu = 1.0 + (p.err + q.err);
+          status = uq * mu < pp ? kAccept : (uq < pp * mu ? kUnclear : kReject);
+          if (pp == 0.0) status = kReject;
+          out = (float)(lp * kLn2F64);
+        }
+      }
+      const uint64_t stops = __ballot(status != kAccept);
+      const int first = stops ? __builtin_ctzll(stops) : 64;
+      if (write && in && lane < first) {
+        a.tokens[(int64_t)b * (a.D + 1) + i] = x;
+        a.logp[(int64_t)b * (a.D + 1) + i] = out;
+      }
+      status = __shfl(status, first & 63, 64);
+      if (lane == 0) {
+        st.from = from;
+        st.stop = stops ? Stop{from + first, status} : Stop{min(from + kWindow, n), kAccept};
       }
     }
-    const uint64_t stops = __ballot(status != kAccept);
-    const int stop = stops ? __builtin_ctzll(stops) : 64;
-    if (write && i < n && lane < stop) {
-      a.tokens[(int64_t)b * (a.D + 1) + i] = x;
-      a.logp[(int64_t)b * (a.D + 1) + i] = out;
-    }
-    if (stop < 64) return {i0 + stop, __shfl(status, stop, 64)};
+    __syncthreads();
+    const Stop s = st.stop;
+    if (s.status != kAccept || s.pos == n) return s;
   }
-  return {n, kAccept};
 }
 
 // ------------------------------------------------------------------ statistics
@@ -159,7 +191,7 @@ __global__ __launch_bounds__(kStatsNT) void verify_stats(VerifyArgs a, int i0, i
   constexpr int U = 8;
   constexpr int NW = NT / 64;
   __shared__ double red[3 * NW];
-  __shared__ int alive;
+  __shared__ StopState st;
   const int tid = threadIdx.x;
   const int kinds = a.draft ? 2 : 1;
   const float L = (float)a.t2e;
@@ -180,13 +212,8 @@ __global__ __launch_bounds__(kStatsNT) void verify_stats(VerifyArgs a, int i0, i
 #pragma unroll
     for (int u = 0; u < U; ++u) load16<kAuxLast>(r[u], rz, tid * 16, u * NT * 16);
     if (i0 > 0) {
-      __syncthreads();                               // the last item's flag is read
-      if (tid < 64) {
-        const int s = first_stop<Tin>(a, b, 0, i0, false).status;
-        if (tid == 0) alive = s == kAccept || s == kUnclear;
-      }
-      __syncthreads();
-      if (!alive) continue;
+      const int s = first_stop<Tin, NT>(a, b, 0, i0, false, st).status;
+      if (s == kReject || s == kBadRow) continue;
     }
     float N = -INFINITY, m = -INFINITY;              // 2^N s so far; the largest logit
     double s = 0.0;
@@ -353,7 +380,7 @@ __global__ __launch_bounds__(kCellNT) void verify_cells(VerifyArgs a) {
   constexpr int NW = kCellNT / 64;
   __shared__ double table[kExpTable];
   __shared__ double red[NW];
-  __shared__ Stop stop_s;
+  __shared__ StopState st;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -365,13 +392,7 @@ __global__ __launch_bounds__(kCellNT) void verify_cells(VerifyArgs a) {
     // where the sequence stops; every workgroup of a sequence comes to the same answer
     VerifyDraw d{};
     for (int from = 0;;) {
-      __syncthreads();                               // the table is written, stop_s is read
-      if (wave == 0) {
-        const Stop s = first_stop<Tin>(a, b, from, n, part == 0);
-        if (tid == 0) stop_s = s;
-      }
-      __syncthreads();
-      const Stop s = stop_s;
+      const Stop s = first_stop<Tin, kCellNT>(a, b, from, n, part == 0, st);
       d.pos = s.pos;
       d.mode = s.status == kBadRow ? kDrawBad
                : s.pos == n        ? kDrawTarget
@@ -401,9 +422,9 @@ __global__ __launch_bounds__(kCellNT) void verify_cells(VerifyArgs a) {
       from = s.pos + 1;
     }
     if (d.mode != kDrawBad) {
-      const RowNorm p = row_norm(a, b, d.pos, 0);
+      const RowNorm p = st.norm[0][d.pos - st.from];
       RowNorm q{};
-      if (d.mode == kDrawResidual) q = row_norm(a, b, d.pos, 1);
+      if (d.mode == kDrawResidual) q = st.norm[1][d.pos - st.from];
       d.far = p.far || q.far;
       if (p.bad || q.bad) d.mode = kDrawBad;
       if (d.far && d.mode != kDrawBad) {             // uniform
@@ -498,15 +519,29 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
       }
       continue;
     }
-    const VerifyCell* cell = a.cell + b * a.cells;
+    const VerifyCell* cells = a.cell + b * a.cells;
     const int run = (a.cells + NT - 1) / NT;         // cells per thread, consecutive
     const int r0 = min(tid * run, a.cells), r1 = min(r0 + run, a.cells);
+    // the first of them in registers, loaded together (all of them up to V = 2^20 bf16, 2^19 fp32)
+    constexpr int R = 4;
+    VerifyCell own_cells[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) own_cells[k] = r0 + k < r1 ? cells[r0 + k] : VerifyCell{0.0, 0.0, 0.0, 0.0};
+    // f(cell, its sums) over this thread's cells, until it returns true
+    auto each = [&](auto&& f) {
+      bool done = false;
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+        if (!done && r0 + k < r1) done = f(r0 + k, own_cells[k]);
+      for (int c = r0 + R; c < r1 && !done; ++c) done = f(c, cells[c]);
+    };
     // p's and q's exact totals: the scale that q has to have against p
     double tp = 0.0, tq = 0.0;
-    for (int c = r0; c < r1; ++c) {
-      tp += cell[c].p;
-      tq += cell[c].q;
-    }
+    each([&](int, const VerifyCell& c) {
+      tp += c.p;
+      tq += c.q;
+      return false;
+    });
     tp = wave_sum_f64(tp);
     tq = wave_sum_f64(tq);
     if (lane == 0) {
@@ -527,15 +562,17 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
     bool residual = d.mode == kDrawResidual;
     const double scale = residual ? tp / tq : 0.0;   // of q; phi is the scale the cells used
     bool from_p = d.mode == kDrawTarget;
-    auto weight = [&](int c) {
-      if (from_p) return cell[c].p;
-      const double r = cell[c].r - (scale - d.phi) * cell[c].slope;
-      return residual ? fmax(r, 0.0) : r;
+    auto weight = [&](const VerifyCell& c) {
+      if (from_p) return c.p;
+      return residual ? fmax(c.r - (scale - d.phi) * c.slope, 0.0) : c.r;
     };
     double before = 0.0, total = 0.0, own = 0.0;     // the cells before this thread's, all, its own
     for (;;) {
       own = 0.0;
-      for (int c = r0; c < r1; ++c) own += weight(c);
+      each([&](int, const VerifyCell& c) {
+        own += weight(c);
+        return false;
+      });
       double incl = own;
 #pragma unroll
       for (int off = 1; off < 64; off <<= 1) {
@@ -560,18 +597,19 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
     int hit_cell = a.cells;
     double hit_before = before;
     {
-      double c = before;
-      for (int i = r0; i < r1; ++i) {
-        const double w = weight(i);
+      double sum = before;
+      each([&](int i, const VerifyCell& c) {
+        const double w = weight(c);
         if (w > 0.0) atomicMax(&last_s, i);
-        if (c + w > goal && w > 0.0) {
+        if (sum + w > goal && w > 0.0) {
           atomicMin(&found_s, i);
           hit_cell = i;
-          hit_before = c;
-          break;
+          hit_before = sum;
+          return true;
         }
-        c += w;
-      }
+        sum += w;
+        return false;
+      });
     }
     __syncthreads();
     const int found = found_s < a.cells ? found_s : last_s;   // total > 0: some weight is positive
