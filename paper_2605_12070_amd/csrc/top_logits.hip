@@ -4,15 +4,17 @@
 // A bound that at least k entries reach lets almost every entry be dropped with one comparison. The
 // k-th largest of the threads' running maxima is such a bound: k different entries reach it. A
 // workgroup streams a row in tiles of U 16-byte chunks per thread; after the first tile, and each
-// time the part read has doubled, it takes that bound from the maxima so far, and entries that reach
-// the bound of their time are kept in LDS (k ln(tiles) of them in random order). At the end the kept
-// ones are ranked by counting, which needs no barrier. What the fast path cannot hold (long runs of
+// time the part read has doubled, it takes that bound from the maxima so far, and chunks with an entry
+// that reaches the bound of their time are kept in LDS (about k (1 + ln tiles) of them in random
+// order). At the end the kept chunks' entries that reach the last bound are ranked by counting, which
+// needs no barrier. What the fast path cannot hold (long runs of
 // equal values, a row with NaN or infinities, fewer than k finite entries) is selected exactly by
 // radix passes over the row.
 #include "top_logits.h"
 
 #include <algorithm>
 
+#include "dppo.h"
 #include "dppo_device.h"
 #include "row_split.h"
 
@@ -21,8 +23,9 @@ namespace dppo {
 namespace {
 
 constexpr int kTopU = 8;         // 16-byte chunks per thread in flight
-// Kept entries. A row whose maxima are too few for a bound is kept whole: fewer than 256 chunks of 8
-// entries and two ends.
+// Kept chunks, and entries of them that reach the final bound. A row whose maxima are too few for a
+// bound is kept whole: fewer than 256 chunks of 8 entries and two ends.
+constexpr int kTopChunks = 1056;
 constexpr int kTopCap = 2112;
 constexpr int kTopRank = 512;    // more than these are thinned out before the ranking
 
@@ -79,17 +82,17 @@ __device__ __forceinline__ void put(const TopArgs& a, int64_t row, int part, int
 }
 
 template <typename Tin, int NT>
-__global__ __launch_bounds__(NT) void top_rows(TopArgs a) {
+__global__ __launch_bounds__(NT, 6) void top_rows(TopArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int U = kTopU;
   constexpr int NW = NT / 64;
+  __shared__ u32x4 chunk[kTopChunks];     // kept chunks; later the thinned-out entries
+  __shared__ int chunk_at[kTopChunks];    // entry that a kept chunk starts at
   __shared__ uint64_t cand[kTopCap];
-  __shared__ uint64_t kept[kTopCap];
   __shared__ uint32_t tkey[NT];
   __shared__ float red[2 * NW];
   __shared__ int wcount[NW];
-  __shared__ int hist[256];
-  __shared__ int count, kcount;
+  __shared__ int chunks, count, kcount;
   __shared__ uint32_t bound_s;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -113,7 +116,7 @@ __global__ __launch_bounds__(NT) void top_rows(TopArgs a) {
     const int ei = tid < le ? tid : sp.lead + sp.nfull * E + (tid - le);
     const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + first, n * 16);
     __syncthreads();                       // the last item's LDS is free
-    if (tid == 0) count = kcount = 0;
+    if (tid == 0) chunks = count = kcount = 0;
 
     uint32_t r[U][4];
 #pragma unroll
@@ -160,11 +163,13 @@ __global__ __launch_bounds__(NT) void top_rows(TopArgs a) {
       if (slot < kTopCap) cand[slot] = composite(x, idx);
     };
     float bound = 0.0f;
-    auto test = [&](const float (&x)[E], float cm, int c) {
+    auto test = [&](const uint32_t (&w)[4], float cm, int c) {
       if (cm >= bound) {
-#pragma unroll
-        for (int j = 0; j < E; ++j)
-          if (x[j] >= bound) push(x[j], first + c * E + j);
+        const int slot = atomicAdd(&chunks, 1);
+        if (slot < kTopChunks) {
+          chunk[slot] = u32x4{w[0], w[1], w[2], w[3]};
+          chunk_at[slot] = first + c * E;
+        }
       }
     };
     // first tile: the maxima, their bound, then the entries that reach it
@@ -173,17 +178,16 @@ __global__ __launch_bounds__(NT) void top_rows(TopArgs a) {
       if (u * NT >= n) break;              // uniform
       float x[E];
       unpack<Tin>(r[u], x);
-      if (u * NT + tid < n) add(x, max_of(x));
+      if (tid < n - u * NT) add(x, max_of(x));
     }
     bound = update_bound();
-    if (edge && xe >= bound) push(xe, ei);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (u * NT >= n) break;
       float x[E];
       unpack<Tin>(r[u], x);
+      if (tid < n - u * NT) test(r[u], max_of(x), u * NT + tid);
       if ((U + u) * NT < n) load16<kAuxLast>(r[u], rz, tid * 16, (U + u) * NT * 16);
-      if (u * NT + tid < n) test(x, max_of(x), u * NT + tid);
     }
     int t = 1;
     for (int b = U * NT; b < n; b += U * NT, ++t) {
@@ -192,23 +196,40 @@ __global__ __launch_bounds__(NT) void top_rows(TopArgs a) {
         if (b + u * NT >= n) break;
         float x[E];
         unpack<Tin>(r[u], x);
-        if (b + (U + u) * NT < n) load16<kAuxLast>(r[u], rz, tid * 16, (b + (U + u) * NT) * 16);
-        if (b + u * NT + tid < n) {
+        if (tid < n - b - u * NT) {
           const float cm = max_of(x);
           add(x, cm);
-          test(x, cm, b + u * NT + tid);
+          test(r[u], cm, b + u * NT + tid);
         }
+        if (b + (U + u) * NT < n) load16<kAuxLast>(r[u], rz, tid * 16, (b + (U + u) * NT) * 16);
       }
       if ((t & (t + 1)) == 0 && b + U * NT < n) bound = update_bound();
     }
-    block_merge_ns_int<NT>(N, S, red);     // its barrier also makes `count` final
+    if (n > U * NT) bound = update_bound();
+    block_merge_ns_int<NT>(N, S, red);     // its barrier also makes the kept chunks final
+    // the entries that reach the last bound
+    const int nc = chunks;
+    if (edge && xe >= bound) push(xe, ei);
+    for (int i = tid; i < min(nc, kTopChunks); i += NT) {
+      const u32x4 v = chunk[i];
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      const int at = chunk_at[i];
+      float x[E];
+      unpack<Tin>(w, x);
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (x[j] >= bound) push(x[j], at + j);
+    }
+    __syncthreads();
     int m = count;
     const uint64_t* list = cand;
     const int kk = k < e1 - e0 ? k : e1 - e0;
-    if (m > kTopCap || m < kk || !(S < INFINITY)) {
+    if (nc > kTopChunks || m > kTopCap || m < kk || !(S < INFINITY)) {
       // exact: the key of the kk-th entry by radix passes, then everything above it and the first
       // of its equals
       __syncthreads();
+      int* hist = (int*)tkey;
+      static_assert(NT >= 256);
       uint32_t prefix = 0, mask = 0;
       int need = kk;
       for (int shift = 24; shift >= 0; shift -= 8) {
@@ -269,6 +290,8 @@ __global__ __launch_bounds__(NT) void top_rows(TopArgs a) {
           reach = c;
         }
       }
+      uint64_t* kept = (uint64_t*)chunk;
+      static_assert(sizeof(chunk) >= 8 * kTopCap);
       for (int i = tid; i < m; i += NT) {
         const uint64_t c = cand[i];
         if ((uint32_t)(c >> 32) >= b) kept[atomicAdd(&kcount, 1)] = c;
@@ -295,46 +318,49 @@ __global__ __launch_bounds__(NT) void top_rows(TopArgs a) {
   }
 }
 
-// Joins a row's parts: an entry's rank is its place in its own part's list and the number of larger
-// ones in each other list (a binary search: the lists are sorted).
-constexpr int kJoinNT = 256;
+// Joins a row's parts. Their lists are sorted, so the least of the parts' ceil(k / parts)-th entries is
+// a bound that at least k entries reach; those are ranked by counting.
+constexpr int kJoinNT = 512;
 constexpr int kTopParts = 16;
 
 __global__ __launch_bounds__(kJoinNT) void top_join(TopArgs a) {
-  __shared__ uint64_t list[kTopParts * 256];
+  __shared__ uint64_t list[kTopParts * DPPO_MAX_TOP];
+  __shared__ uint64_t kept[kTopParts * DPPO_MAX_TOP];
+  __shared__ int count;
   const int tid = threadIdx.x;
   const int k = a.k;
   const int m = a.parts * k;
+  const int share = (k + a.parts - 1) / a.parts;
   for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
     __syncthreads();
+    if (tid == 0) count = 0;
     for (int i = tid; i < m; i += kJoinNT) list[i] = a.cand[row * m + i];
+    float N = -INFINITY, S = 0.0f;
+    if (tid == 0)
+      for (int p = 0; p < a.parts; ++p)
+        merge_ns_int(N, S, a.part[2 * (row * a.parts + p)], a.part[2 * (row * a.parts + p) + 1]);
     __syncthreads();
+    uint64_t bound = list[share - 1];
+    for (int p = 1; p < a.parts; ++p) {
+      const uint64_t c = list[p * k + share - 1];
+      bound = c < bound ? c : bound;
+    }
     for (int i = tid; i < m; i += kJoinNT) {
       const uint64_t c = list[i];
-      if (c == 0) continue;
-      const int own = i / k;
-      int rank = i - own * k;
-      for (int p = 0; p < a.parts && rank < k; ++p) {
-        if (p == own) continue;
-        int lo = 0, hi = k;                // entries [0, lo) are larger than c
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (list[p * k + mid] > c) lo = mid + 1;
-          else hi = mid;
-        }
-        rank += lo;
-      }
+      if (c >= bound && c != 0) kept[atomicAdd(&count, 1)] = c;
+    }
+    __syncthreads();
+    const int n = count;
+    for (int i = tid; i < n; i += kJoinNT) {
+      const uint64_t c = kept[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += kept[j] > c;
       if (rank < k) {
         a.values[row * k + rank] = key_value((uint32_t)(c >> 32));
         a.ids[row * k + rank] = (int32_t)~(uint32_t)c;
       }
     }
-    if (tid == 0) {
-      float N = -INFINITY, S = 0.0f;
-      for (int p = 0; p < a.parts; ++p)
-        merge_ns_int(N, S, a.part[2 * (row * a.parts + p)], a.part[2 * (row * a.parts + p) + 1]);
-      a.lse[row] = (N == -INFINITY) ? __builtin_nanf("") : (N + log2f(S)) * kLn2;
-    }
+    if (tid == 0) a.lse[row] = (N == -INFINITY) ? __builtin_nanf("") : (N + log2f(S)) * kLn2;
   }
 }
 
