@@ -238,7 +238,7 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
           if (e >= 0 && e < E) f(j, e);
         }
       };
-      float N = -INFINITY, S = 0.0f;
+      float N = kNoShift, S = 0.0f;
       auto add = [&](float (&x)[E], int slot) {
         if (slots >> (slot & 31) & 1u)
           held(slot, [&](int, int e) {
@@ -248,12 +248,7 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
         float cm = max3(x[0], x[1], x[2]);
         if constexpr (E == 8) cm = max3(cm, max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
         else cm = fmaxf(cm, x[3]);
-        const float nc = __builtin_ceilf(cm * L);
-        const float sh = (nc == -INFINITY) ? 0.0f : nc;
-        float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < E; ++i) s += exp2_hw(__builtin_fmaf(x[i], L, -sh));
-        merge_ns_int(N, S, nc, s);
+        add_logits(N, S, x, cm, L);
       };
       const __amdgpu_buffer_rsrc_t rz = row_rsrc(zrow + sp.lead, nfull * 16);
       // the chunks past the registers
@@ -289,14 +284,14 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
         bool own = false;
         if (edge_held)
           for (int j = head; j >= 0; j = rec.next[j]) own |= rec.id[j] == ei;
-        const float x = own ? -INFINITY : xe;
-        const float nc = __builtin_ceilf(x * L);
-        merge_ns_int(N, S, nc, nc == -INFINITY ? 0.0f : exp2_hw(__builtin_fmaf(x, L, -nc)));
+        const float x[1] = {own ? -INFINITY : xe};
+        add_logits(N, S, x, x[0], L);
       }
       if (tid < a.k) {
         rm.value[tid] = tv;
         rm.z[tid] = tz;
       }
+      N = shift_of(N);
       block_merge_ns_int<NT>(N, S, red[parity]);
       if (tid < 64) record_math(a, row, scale * (a.tscale ? uload(a.tscale + row) : 1.0f), N, S, rec, rm);
       if (tid == 0) a.flags[row] = (uint8_t)DPPO_FLAG_VALID;

@@ -91,6 +91,27 @@ __device__ __forceinline__ void merge_ns_int(float& n, float& s, float n2, float
   n = N;
 }
 
+// Adds E logits with maximum cm to a running sum 2^n s, in log2 units of z L. The shift n is an
+// integer and the running maximum's, so its change scales s exactly, and a chunk costs one more
+// exponential (merge_ns_int, whose chunks have shifts of their own, two). n starts at kNoShift; logits
+// whose z L lies below it count as -inf.
+constexpr float kNoShift = -3.0e38f;
+template <int E, typename Sum>
+__device__ __forceinline__ void add_logits(float& n, Sum& s, const float (&x)[E], float cm, float L) {
+  static_assert(E == 1 || E == 4 || E == 8);
+  const float N = fmaxf(n, __builtin_ceilf(cm * L));
+  float e[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) e[j] = exp2_hw(__builtin_fmaf(x[j], L, -N));
+  float c = e[0];
+  if constexpr (E == 8) c = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+  if constexpr (E == 4) c = (e[0] + e[1]) + (e[2] + e[3]);
+  s = s * (Sum)exp2_hw(n - N) + (Sum)c;
+  n = N;
+}
+// The sum's shift, or -inf while nothing has been added.
+__device__ __forceinline__ float shift_of(float n) { return n == kNoShift ? -INFINITY : n; }
+
 template <int CTRL>
 __device__ __forceinline__ float dpp_f(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL,

@@ -121,14 +121,9 @@ __global__ __launch_bounds__(NT, 6) void top_rows(TopArgs a) {
     uint32_t r[U][4];
 #pragma unroll
     for (int u = 0; u < U; ++u) load16<kAuxLast>(r[u], rz, tid * 16, u * NT * 16);
-    float N = -INFINITY, S = 0.0f, tmax = -INFINITY;
+    float N = kNoShift, S = 0.0f, tmax = -INFINITY;
     auto add = [&](const auto& x, float cm) {
-      const float nc = __builtin_ceilf(cm * L);
-      const float sh = (nc == -INFINITY) ? 0.0f : nc;
-      float s = 0.0f;
-#pragma unroll
-      for (int j = 0; j < (int)(sizeof(x) / 4); ++j) s += exp2_hw(__builtin_fmaf(x[j], L, -sh));
-      merge_ns_int(N, S, nc, s);
+      add_logits(N, S, x, cm, L);
       tmax = fmaxf(tmax, cm);
     };
     float xe = -INFINITY;
@@ -206,6 +201,7 @@ __global__ __launch_bounds__(NT, 6) void top_rows(TopArgs a) {
       if ((t & (t + 1)) == 0 && b + U * NT < n) bound = update_bound();
     }
     if (n > U * NT) bound = update_bound();
+    N = shift_of(N);
     block_merge_ns_int<NT>(N, S, red);     // its barrier also makes the kept chunks final
     // the entries that reach the last bound
     const int nc = chunks;

@@ -215,24 +215,11 @@ __global__ __launch_bounds__(kStatsNT) void verify_stats(VerifyArgs a, int i0, i
       const int s = first_stop<Tin, NT>(a, b, 0, i0, false, st).status;
       if (s == kReject || s == kBadRow) continue;
     }
-    float N = -INFINITY, m = -INFINITY;              // 2^N s so far; the largest logit
+    float N = kNoShift, m = -INFINITY;               // 2^N s so far; the largest logit
     double s = 0.0;
     auto add = [&](const auto& x) {
       const float cm = max_of(x);
-      const float nc = __builtin_ceilf(cm * L);
-      const float sh = (nc == -INFINITY) ? 0.0f : nc;
-      float e[sizeof(x) / 4];
-#pragma unroll
-      for (int j = 0; j < (int)(sizeof(x) / 4); ++j) e[j] = exp2_hw(__builtin_fmaf(x[j], L, -sh));
-      float cs = e[0];
-      if constexpr (sizeof(x) == 32) cs = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-      if constexpr (sizeof(x) == 16) cs = (e[0] + e[1]) + (e[2] + e[3]);
-      // integer shifts: the scales are exact
-      const float M = fmaxf(N, nc);
-      const float fa = (N == M) ? 1.0f : exp2_hw(N - M);
-      const float fb = (nc == M) ? 1.0f : exp2_hw(nc - M);
-      s = s * (double)fa + (double)(cs * fb);
-      N = M;
+      add_logits(N, s, x, cm, L);
       m = fmaxf(m, cm);
     };
     if (part == 0 && tid < sp.nedge) {
@@ -255,7 +242,7 @@ __global__ __launch_bounds__(kStatsNT) void verify_stats(VerifyArgs a, int i0, i
     m = wave_max(m);
     __syncthreads();                                 // the last item's partials are read
     if ((tid & 63) == 0) {
-      red[tid >> 6] = M;
+      red[tid >> 6] = shift_of(M);
       red[NW + (tid >> 6)] = s;
       red[2 * NW + (tid >> 6)] = m;
     }
