@@ -22,7 +22,10 @@ namespace dppo {
 
 namespace {
 
-constexpr int kTopU = 8;         // 16-byte chunks per thread in flight
+// 16-byte chunks per thread in flight. Four leave 64 registers and LDS for 32 waves per CU: against
+// eight (24 waves) T = 8192, V = 151936 bf16, k = 64 497 -> 436 us, T = 2048, V = 50257 fp32, k = 128
+// 120 -> 94 us.
+constexpr int kTopU = 4;
 // Kept chunks, and entries of them that reach the final bound. A row whose maxima are too few for a
 // bound is kept whole: fewer than 256 chunks of 8 entries and two ends.
 constexpr int kTopChunks = 1056;
@@ -82,7 +85,7 @@ __device__ __forceinline__ void put(const TopArgs& a, int64_t row, int part, int
 }
 
 template <typename Tin, int NT>
-__global__ __launch_bounds__(NT, 6) void top_rows(TopArgs a) {
+__global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int U = kTopU;
   constexpr int NW = NT / 64;
@@ -92,7 +95,7 @@ __global__ __launch_bounds__(NT, 6) void top_rows(TopArgs a) {
   __shared__ uint32_t tkey[NT];
   __shared__ float red[2 * NW];
   __shared__ int wcount[NW];
-  __shared__ int chunks, count, kcount;
+  __shared__ int chunks, chunks_s, count, kcount;
   __shared__ uint32_t bound_s;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -148,7 +151,10 @@ __global__ __launch_bounds__(NT, 6) void top_rows(TopArgs a) {
           for (int j = 0; j < NW; ++j) c += __popcll(__ballot(key[j] >= t));
           if (c >= k) b = t;
         }
-        if (lane == 0) bound_s = b > kKeyLowest ? b : kKeyLowest;
+        if (lane == 0) {
+          bound_s = b > kKeyLowest ? b : kKeyLowest;
+          chunks_s = chunks;               // between the barriers: nothing is kept meanwhile
+        }
       }
       __syncthreads();
       return key_value(bound_s);
@@ -158,15 +164,17 @@ __global__ __launch_bounds__(NT, 6) void top_rows(TopArgs a) {
       if (slot < kTopCap) cand[slot] = composite(x, idx);
     };
     float bound = 0.0f;
-    auto test = [&](const uint32_t (&w)[4], float cm, int c) {
+    bool lost = false;                     // the list of chunks was full
+    auto keep = [&](const uint32_t (&w)[4], float cm, int at) {
       if (cm >= bound) {
         const int slot = atomicAdd(&chunks, 1);
         if (slot < kTopChunks) {
           chunk[slot] = u32x4{w[0], w[1], w[2], w[3]};
-          chunk_at[slot] = first + c * E;
+          chunk_at[slot] = at;
         }
       }
     };
+    auto test = [&](const uint32_t (&w)[4], float cm, int c) { keep(w, cm, first + c * E); };
     // first tile: the maxima, their bound, then the entries that reach it
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -198,7 +206,33 @@ __global__ __launch_bounds__(NT, 6) void top_rows(TopArgs a) {
         }
         if (b + (U + u) * NT < n) load16<kAuxLast>(r[u], rz, tid * 16, (b + (U + u) * NT) * 16);
       }
-      if ((t & (t + 1)) == 0 && b + U * NT < n) bound = update_bound();
+      if ((t & (t + 1)) == 0 && b + U * NT < n) {
+        bound = update_bound();
+        // drop kept chunks that no longer reach the bound before the list gets full
+        const int have = chunks_s;
+        if (have > kTopChunks / 2) {         // uniform
+          lost |= have > kTopChunks;
+          // in place: a step's chunks are read before any is kept, at places read already
+          for (int i = 0; i < min(have, kTopChunks); i += NT) {
+            const int j = i + tid;
+            u32x4 v = {0u, 0u, 0u, 0u};
+            int at = -1;
+            if (j < min(have, kTopChunks)) {
+              v = chunk[j];
+              at = chunk_at[j];
+            }
+            __syncthreads();
+            if (i == 0) {
+              if (tid == 0) chunks = 0;
+              __syncthreads();
+            }
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            float x[E];
+            unpack<Tin>(w, x);
+            if (at >= 0) keep(w, max_of(x), at);
+          }
+        }
+      }
     }
     if (n > U * NT) bound = update_bound();
     N = shift_of(N);
@@ -220,7 +254,7 @@ __global__ __launch_bounds__(NT, 6) void top_rows(TopArgs a) {
     int m = count;
     const uint64_t* list = cand;
     const int kk = k < e1 - e0 ? k : e1 - e0;
-    if (nc > kTopChunks || m > kTopCap || m < kk || !(S < INFINITY)) {
+    if (lost || nc > kTopChunks || m > kTopCap || m < kk || !(S < INFINITY)) {
       // exact: the key of the kk-th entry by radix passes, then everything above it and the first
       // of its equals
       __syncthreads();

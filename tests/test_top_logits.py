@@ -105,3 +105,26 @@ def test_the_same_bits_again():
     for _ in range(3):
         b = P.top_logits(z, 256)
         assert torch.equal(a.values, b.values) and torch.equal(a.ids, b.ids) and torch.equal(a.lse, b.lse)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,V,k", [(40, 262144, 256), (30, 151936, 256), (20, 100003, 129)])
+def test_wide_records_of_long_rows(dtype, T, V, k):
+    """The list of kept chunks is thinned out on the way: against torch's own order of the values
+    (distinct keys), which is quicker than the oracle's."""
+    print(f"[case] top wide {dtype} T={T} V={V} k={k}", flush=True)
+    z = torch.empty(T, V, dtype=dtype, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(k)
+    for t in range(T):
+        z[t] = (3.0 * torch.randn(V, generator=g, device=DEV)).to(dtype)
+    z[1] = torch.sort(z[1].float()).values.to(dtype)
+    z[2] += torch.linspace(0, 20, V, device=DEV).to(dtype)
+    z[3, V // 2:] += 15
+    r = P.top_logits(z, k)
+    bits = (z.float() + 0.0).view(torch.int32)
+    key = ((bits ^ ((bits >> 31) & 0x7FFFFFFF)).long() << 32) + torch.arange(V - 1, -1, -1, device=DEV)
+    ids = V - 1 - (torch.topk(key, k, dim=1).values & 0xFFFFFFFF)
+    assert torch.equal(r.ids.long(), ids)
+    assert torch.equal(r.values, z.float().gather(1, ids))
+    lse = torch.logsumexp(z.double(), 1)
+    assert bool(((r.lse - lse).abs() <= LSE * lse.abs().clamp_min(1)).all())
