@@ -6,8 +6,7 @@
 // workgroup streams a row in tiles of U 16-byte chunks per thread; after the first tile, and each
 // time the part read has doubled, it takes that bound from the maxima so far, and chunks with an entry
 // that reaches the bound of their time are kept in LDS (about k (1 + ln tiles) of them in random
-// order). At the end the kept chunks' entries that reach the last bound are ranked by counting, which
-// needs no barrier. What the fast path cannot hold (long runs of
+// order). At the end the kept chunks' entries that reach the last bound are ranked by counting. What the fast path cannot hold (long runs of
 // equal values, a row with NaN or infinities, fewer than k finite entries) is selected exactly by
 // radix passes over the row.
 #include "top_logits.h"
@@ -81,6 +80,103 @@ __device__ __forceinline__ void put(const TopArgs& a, int64_t row, int part, int
   } else {
     a.values[row * a.k + rank] = key_value((uint32_t)(c >> 32));
     a.ids[row * a.k + rank] = (int32_t)~(uint32_t)c;
+  }
+}
+
+// Sorts list[0, n), n <= 64 R, best first, by one wave: a bitonic network over R entries per lane in
+// registers (place lane R + r). Ranking by counting took n / 64 passes over the list instead: at k =
+// 250 most of a short row's time.
+template <int R>
+__device__ __noinline__ void sort_list(uint64_t* list, int n) {
+  const int lane = threadIdx.x & 63;
+  uint64_t v[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) v[r] = lane * R + r < n ? list[lane * R + r] : 0;
+#pragma unroll
+  for (int size = 2; size <= 64 * R; size *= 2) {
+#pragma unroll
+    for (int stride = size / 2; stride > 0; stride /= 2) {
+      if (stride >= R) {
+        const int mask = stride / R;
+        const bool lower = (lane & mask) == 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const bool down = ((lane * R + r) & size) == 0;      // this run of `size` falls
+          const uint64_t o = __shfl_xor(v[r], mask, 64);
+          v[r] = (v[r] > o) == (lower == down) ? v[r] : o;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (r & stride) continue;
+          const bool down = ((lane * R + r) & size) == 0;
+          const uint64_t x = v[r], y = v[r + stride];
+          const bool swap = (x > y) != down;
+          v[r] = swap ? y : x;
+          v[r + stride] = swap ? x : y;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (lane * R + r < n) list[lane * R + r] = v[r];
+}
+constexpr int kSortMost = 512;
+__device__ __forceinline__ void sort_list(uint64_t* list, int n) {
+  if (n <= 64) sort_list<1>(list, n);
+  else if (n <= 128) sort_list<2>(list, n);
+  else if (n <= 256) sort_list<4>(list, n);
+  else sort_list<8>(list, n);
+}
+
+// Exactly the kk best of the entries [e0, e1) of z into cand, in any order: the key of the kk-th by radix
+// passes over the row, then everything above it and the first of its equals. By the whole workgroup,
+// behind a barrier; hist holds 256 counts, wcount one per wave.
+template <typename Tin, int NT>
+__device__ __noinline__ void select_exact(const Tin* z, int e0, int e1, int kk, uint64_t* cand, int* count,
+                                          int* hist, int* wcount) {
+  constexpr int NW = NT / 64;
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = tid >> 6;
+  uint32_t prefix = 0, mask = 0;
+  int need = kk;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = tid; i < 256; i += NT) hist[i] = 0;
+    __syncthreads();
+    for (int e = e0 + tid; e < e1; e += NT) {
+      const uint32_t key = value_key(entry_value(z, e));
+      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1);
+    }
+    __syncthreads();
+    int bin = 255;
+    for (int above = hist[bin]; above < need; above = hist[bin]) {
+      need -= above;
+      --bin;
+    }
+    prefix |= (uint32_t)bin << shift;
+    mask |= 255u << shift;
+    __syncthreads();
+  }
+  if (tid == 0) *count = 0;
+  int before = 0;                          // equals before this step
+  __syncthreads();
+  for (int base = e0; base < e1; base += NT) {
+    const int e = base + tid;
+    const float x = e < e1 ? entry_value(z, e) : 0.0f;
+    const uint32_t key = value_key(x);
+    const bool tie = e < e1 && key == prefix;
+    const uint64_t ties = __ballot(tie);
+    if (lane == 0) wcount[wave] = __popcll(ties);
+    __syncthreads();
+    int at = before + __popcll(ties & ((1ull << lane) - 1ull));
+    for (int w = 0; w < NW; ++w) {
+      if (w < wave) at += wcount[w];
+      before += wcount[w];
+    }
+    if ((e < e1 && key > prefix) || (tie && at < need)) cand[atomicAdd(count, 1)] = composite(x, e);
+    __syncthreads();
   }
 }
 
@@ -252,53 +348,12 @@ __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
     }
     __syncthreads();
     int m = count;
-    const uint64_t* list = cand;
+    uint64_t* list = cand;
     const int kk = k < e1 - e0 ? k : e1 - e0;
     if (lost || nc > kTopChunks || m > kTopCap || m < kk || !(S < INFINITY)) {
-      // exact: the key of the kk-th entry by radix passes, then everything above it and the first
-      // of its equals
       __syncthreads();
-      int* hist = (int*)tkey;
       static_assert(NT >= 256);
-      uint32_t prefix = 0, mask = 0;
-      int need = kk;
-      for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += NT) hist[i] = 0;
-        __syncthreads();
-        for (int e = e0 + tid; e < e1; e += NT) {
-          const uint32_t key = value_key(entry_value(z, e));
-          if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1);
-        }
-        __syncthreads();
-        int bin = 255;
-        for (int above = hist[bin]; above < need; above = hist[bin]) {
-          need -= above;
-          --bin;
-        }
-        prefix |= (uint32_t)bin << shift;
-        mask |= 255u << shift;
-        __syncthreads();
-      }
-      if (tid == 0) count = 0;
-      int before = 0;                      // equals before this step
-      __syncthreads();
-      for (int base = e0; base < e1; base += NT) {
-        const int e = base + tid;
-        const float x = e < e1 ? entry_value(z, e) : 0.0f;
-        const uint32_t key = value_key(x);
-        if (e < e1 && key > prefix) push(x, e);
-        const bool tie = e < e1 && key == prefix;
-        const uint64_t ties = __ballot(tie);
-        if (lane == 0) wcount[wave] = __popcll(ties);
-        __syncthreads();
-        int at = before + __popcll(ties & ((1ull << lane) - 1ull));
-        for (int w = 0; w < NW; ++w) {
-          if (w < wave) at += wcount[w];
-          before += wcount[w];
-        }
-        if (tie && at < need) push(x, e);
-        __syncthreads();
-      }
+      select_exact<Tin, NT>(z, e0, e1, kk, cand, &count, (int*)tkey, wcount);
       m = kk;
     } else if (m > kTopRank) {
       // thin out: a key that at least k and, if the keys allow it, at most kTopRank entries reach
@@ -330,6 +385,9 @@ __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
       list = kept;
       m = kcount;
     }
+    // By counting, which all waves share and which needs no registers: with the short rows' sort in this
+    // kernel too its streaming loop has fewer (T = 8192, V = 151936, k = 64 440 -> 513 us; T = 4096,
+    // k = 256 316 -> 288 us).
     for (int i = tid; i < m; i += NT) {
       const uint64_t c = list[i];
       int rank = 0;
@@ -348,8 +406,130 @@ __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
   }
 }
 
+// ---------------------------------------------------------------------------------------
+// Short rows: a wave per row, which stays in registers (M chunks per lane). No barriers, and up to 32
+// rows of a CU in flight: T = 8192, V = 2048 bf16, k = 64 took 93 us with a workgroup per row. The
+// bound is searched over the chunks' maxima (64 M groups), and where that leaves too many entries (few
+// chunks, or k close to their number) over the entries themselves.
+// ---------------------------------------------------------------------------------------
+constexpr int kShortCap = 512;
+constexpr int kShortRows = 512;
+
+template <typename Tin, int M>
+__global__ __launch_bounds__(64) void top_short(TopArgs a) {
+  constexpr int E = 16 / (int)sizeof(Tin);
+  constexpr uint32_t kKeyInf = 0xFF800000u;          // the key of +inf
+  __shared__ uint64_t cand[kShortCap];
+  __shared__ int hist[256];
+  __shared__ int count, wcount;
+  const int lane = threadIdx.x;
+  const uint64_t below = (1ull << lane) - 1ull;
+  const int k = a.k;
+  for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+    const Tin* z = (const Tin*)a.logits + row * a.ld;
+    const RowSplit sp = split_row(z, a.V);
+    const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + sp.lead, sp.nfull * 16);
+    uint32_t r[M][4];
+#pragma unroll
+    for (int m = 0; m < M; ++m) load16<kAuxLast>(r[m], rz, lane * 16, m * 1024);
+    const bool edge = lane < sp.nedge;
+    const int ei = sp.template entry<E>(lane);
+    const float xe = edge ? entry_value(z, ei) : -INFINITY;
+    float N = kNoShift, S = 0.0f;
+    {
+      const float x[1] = {xe};
+      add_logits(N, S, x, xe, a.l2e);
+    }
+    float cm[M];                           // the chunks' maxima
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      cm[m] = -INFINITY;
+      if (m * 64 >= sp.nfull) continue;    // uniform
+      float x[E];
+      unpack<Tin>(r[m], x);
+      if (lane < sp.nfull - m * 64) {
+        cm[m] = max_of(x);
+        add_logits(N, S, x, cm[m], a.l2e);
+      }
+    }
+    N = shift_of(N);
+    wave_merge_ns_int(N, S);
+    auto groups = [&](float f) {
+      int c = __popcll(__ballot(xe >= f));
+#pragma unroll
+      for (int m = 0; m < M; ++m) c += __popcll(__ballot(cm[m] >= f));
+      return c;
+    };
+    // entries that reach f: g(their lanes, value, entry), and how many
+    auto entries = [&](float f, auto&& g) {
+      uint64_t on = __ballot(xe >= f);
+      int c = __popcll(on);
+      g(on, 0, xe, ei);
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        if (__ballot(cm[m] >= f) == 0) continue;
+        float x[E];
+        unpack<Tin>(r[m], x);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          on = __ballot(cm[m] >= f && x[j] >= f);    // a chunk outside the row has cm = -inf
+          g(on, c, x[j], sp.lead + (m * 64 + lane) * E + j);
+          c += __popcll(on);
+        }
+      }
+      return c;
+    };
+    auto none = [](uint64_t, int, float, int) {};
+    // largest key prefix found that enough groups, then entries, reach
+    uint32_t lo = kKeyLowest, hi = kKeyInf;
+    if (groups(key_value(lo)) >= k) {
+      while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        const int c = groups(key_value(mid));
+        if (c < k) {
+          hi = mid;
+        } else {
+          lo = mid;
+          if (c <= k + k / 8 + 2) break;
+        }
+      }
+    }
+    int n = entries(key_value(lo), none);
+    const int most = k + k / 4 + 32;       // at most kShortCap
+    static_assert(DPPO_MAX_TOP + DPPO_MAX_TOP / 4 + 32 <= kShortCap);
+    if (S < INFINITY) {                    // uniform, like all of this
+      hi = kKeyInf;
+      while (n > most && hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        const int c = entries(key_value(mid), none);
+        if (c < k) {
+          hi = mid;
+        } else {
+          lo = mid;
+          n = c;
+        }
+      }
+    }
+    if (!(S < INFINITY) || n > kShortCap || n < k) {
+      __syncthreads();
+      select_exact<Tin, 64>(z, 0, a.V, k, cand, &count, hist, &wcount);
+      n = k;
+    } else {
+      entries(key_value(lo), [&](uint64_t on, int before, float x, int e) {
+        if (on >> lane & 1ull) cand[before + __popcll(on & below)] = composite(x, e);
+      });
+    }
+    __syncthreads();
+    sort_list(cand, n);
+    __syncthreads();
+    for (int i = lane; i < k; i += 64) put(a, row, 0, i, cand[i]);
+    if (lane == 0) a.lse[row] = (N == -INFINITY) ? __builtin_nanf("") : (N + log2f(S)) * kLn2;
+    __syncthreads();                       // cand is read
+  }
+}
+
 // Joins a row's parts. Their lists are sorted, so the least of the parts' ceil(k / parts)-th entries is
-// a bound that at least k entries reach; those are ranked by counting.
+// a bound that at least k entries reach; those are sorted.
 constexpr int kJoinNT = 512;
 constexpr int kTopParts = 16;
 
@@ -381,13 +561,20 @@ __global__ __launch_bounds__(kJoinNT) void top_join(TopArgs a) {
     }
     __syncthreads();
     const int n = count;
-    for (int i = tid; i < n; i += kJoinNT) {
-      const uint64_t c = kept[i];
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += kept[j] > c;
-      if (rank < k) {
-        a.values[row * k + rank] = key_value((uint32_t)(c >> 32));
-        a.ids[row * k + rank] = (int32_t)~(uint32_t)c;
+    auto put = [&](int rank, uint64_t c) {
+      a.values[row * k + rank] = key_value((uint32_t)(c >> 32));
+      a.ids[row * k + rank] = (int32_t)~(uint32_t)c;
+    };
+    if (n <= kSortMost) {
+      if (tid < 64) sort_list(kept, n);
+      __syncthreads();
+      for (int i = tid; i < k; i += kJoinNT) put(i, kept[i]);
+    } else {
+      for (int i = tid; i < n; i += kJoinNT) {
+        const uint64_t c = kept[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += kept[j] > c;
+        if (rank < k) put(rank, c);
       }
     }
     if (tid == 0) a.lse[row] = (N == -INFINITY) ? __builtin_nanf("") : (N + log2f(S)) * kLn2;
@@ -406,6 +593,21 @@ int top_parts(int64_t T, int64_t V, int es) {
 hipError_t launch_top_logits(const TopArgs& a, bool bf16, hipStream_t st) {
   constexpr int NT = 512;
   const int64_t items = (int64_t)a.T * a.parts;
+  const int64_t chunks = (int64_t)a.V * (bf16 ? 2 : 4) / 16;
+  // A wave per row where there are many short ones (against a workgroup per row, us; bf16, T = 8192):
+  // V = 2048, k = 16, 64, 250 23, 26, 53 against 72, 77, 177; V = 8192 63, 76, 112 against 81, 88, 131;
+  // T = 4, V = 8000, k = 20 18 against 11.
+  if (chunks <= 64 * 16 && a.T >= kShortRows) {      // parts is 1: top_parts
+    const unsigned g = (unsigned)std::min<int64_t>(a.T, kLaunchThreads / 64);
+    if (chunks <= 64 * 4) {
+      if (bf16) top_short<uint16_t, 4><<<g, 64, 0, st>>>(a);
+      else top_short<float, 4><<<g, 64, 0, st>>>(a);
+    } else {
+      if (bf16) top_short<uint16_t, 16><<<g, 64, 0, st>>>(a);
+      else top_short<float, 16><<<g, 64, 0, st>>>(a);
+    }
+    return hipGetLastError();
+  }
   const int64_t grid = std::min<int64_t>(items, kLaunchThreads / NT);
   if (bf16) top_rows<uint16_t, NT><<<dim3((unsigned)grid), NT, 0, st>>>(a);
   else top_rows<float, NT><<<dim3((unsigned)grid), NT, 0, st>>>(a);

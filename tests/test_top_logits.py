@@ -27,7 +27,7 @@ def check(z, k, tau=1.0):
     (1, 1, 1), (3, 2, 2), (5, 7, 7), (2, 9, 1), (4, 64, 64), (3, 100, 33), (7, 255, 255), (2, 256, 256),
     (5, 257, 256), (6, 1000, 20), (3, 2055, 256), (3, 2110, 256), (2, 4096, 256), (4, 5001, 128),
     (9, 8191, 17), (3, 16384, 1), (3, 32769, 64), (2, 50257, 128), (2, 151937, 256), (1, 262144, 64),
-    (600, 4100, 8), (2, 300001, 100),
+    (600, 4100, 8), (2, 300001, 100), (700, 1500, 1), (520, 1025, 256), (600, 200, 200), (515, 8191, 100),
 ])
 def test_random_rows(dtype, T, V, k):
     print(f"[case] top {dtype} T={T} V={V} k={k}", flush=True)
@@ -128,3 +128,26 @@ def test_wide_records_of_long_rows(dtype, T, V, k):
     assert torch.equal(r.values, z.float().gather(1, ids))
     lse = torch.logsumexp(z.double(), 1)
     assert bool(((r.lse - lse).abs() <= LSE * lse.abs().clamp_min(1)).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V,k", [(40, 40), (300, 256), (1030, 3), (2051, 64), (4100, 200)])
+def test_many_short_rows(dtype, V, k):
+    """A wave per row: the same row kinds among many rows."""
+    print(f"[case] top short {dtype} V={V} k={k}", flush=True)
+    T = 512 + 9
+    z = rows(T, V, dtype, seed=V, ld=V + 3, offset=1)
+    inf = float("inf")
+    z[0].fill_(2.5)
+    z[1] = (torch.rand(V, generator=torch.Generator().manual_seed(1)) < 0.5).to(dtype).to(DEV)
+    z[2] = torch.sort(z[2].float()).values.to(dtype)
+    z[3, 20:] = -inf
+    z[4].fill_(-inf)
+    z[5, 17:] = torch.finfo(dtype).min
+    z[6, ::2] = 0.0
+    z[6, 1::2] = -0.0
+    z[7, 5] = inf
+    z[8, V - 1] = float("nan")
+    z[9, 3], z[9, 30], z[9, 7] = float("nan"), inf, -inf
+    z[10, V // 2:] += 30
+    check(z, k, tau=0.9)
