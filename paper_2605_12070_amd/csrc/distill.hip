@@ -85,7 +85,7 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
   sq = wave_uniform(wave_sum_f64(sq));
   double c;
   if (a.tlse) {
-    c = (double)a.tlse[row] * kLog2eF64;
+    c = (double)uload(a.tlse + row) * kLog2eF64;
   } else {
     st = wave_uniform(wave_sum_f64(st));
     c = st == 0.0 ? 0.0 : wave_uniform(tm + log2_f64(st));   // 0: an empty record, or one of -inf alone
@@ -136,14 +136,21 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
   }
 }
 
-template <typename Tin, int NT, int NC, int KS>
+// NT threads x NC chunks of a row in registers, KS x NT more in LDS. With PF the row after the next
+// starts early: its first PF x NT chunks go straight to LDS while this row is worked on, the rest to
+// registers once this row's stores are out. Vector memory operations are waited for in the order they
+// were issued, so whatever a row waits for in its middle (the student's logits at the record's tokens,
+// its single entries) is issued before those loads, from ids that were loaded a row earlier.
+template <typename Tin, int NT, int NC, int KS, int PF>
 __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
+  static_assert(PF <= NC && (KS == 0 || PF == 0));
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int U = 4;                     // further chunks per thread in flight
   __shared__ float red[2][2 * (NT / 64)];
   __shared__ Record<NT> recs[2];
   __shared__ RecordMath rm;
   __shared__ u32x4 keep[KS > 0 ? KS * NT : 1];
+  __shared__ u32x4 ahead[PF > 0 ? PF * NT : 1];   // [chunk][thread]: a wave reads what it loaded
   const int tid = threadIdx.x;
   const int V = a.V;
   const float L = a.l2e;
@@ -156,7 +163,36 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
     const RowSplit sp = split_row(z, V);
     const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + sp.lead, rd ? sp.nfull * 16 : 0);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) load16<kAuxLast>(r[c], rz, tid * 16, c * NT * 16);
+    for (int c = PF; c < NC; ++c) load16<kAuxLast>(r[c], rz, tid * 16, c * NT * 16);
+  };
+  auto load_ahead = [&](int64_t row, bool rd) {
+    if constexpr (PF > 0) {
+      const Tin* z = (const Tin*)a.logits + (rd ? row : 0) * a.ld;
+      const RowSplit sp = split_row(z, V);
+      const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + sp.lead, rd ? sp.nfull * 16 : 0);
+      const int wave0 = __builtin_amdgcn_readfirstlane(tid & ~63);
+#pragma unroll
+      for (int c = 0; c < PF; ++c)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            rz, (__attribute__((address_space(3))) void*)&ahead[c * NT + wave0], 16, tid * 16, c * NT * 16, 0, kAuxLast);
+    }
+  };
+  // one entry of a row (0 for e = -1), as bits of a float
+  auto load_one = [&](__amdgpu_buffer_rsrc_t rz, int e) -> uint32_t {
+    const int off = e < 0 ? 0x7fffff00 : e * (int)sizeof(Tin);
+    if constexpr (sizeof(Tin) == 2) return __builtin_amdgcn_raw_buffer_load_b16(rz, off, 0, kAuxKeep);
+    else return __builtin_amdgcn_raw_buffer_load_b32(rz, off, 0, kAuxKeep);
+  };
+  auto value_of = [&](uint32_t w) { return __uint_as_float(sizeof(Tin) == 2 ? w << 16 : w); };
+  // this thread's entry of a row's record
+  int id_next = -1;
+  float tv_next = 0.0f;
+  auto load_entry = [&](int64_t row, bool rd) {
+    const int64_t at = (rd ? row : 0) * a.k;
+    const int bytes = rd ? a.k * 4 : 0;
+    id_next = (int)__builtin_amdgcn_raw_buffer_load_b32(row_rsrc(a.tokens + at, bytes), tid * 4, 0, kAuxKeep);
+    tv_next = __uint_as_float(
+        __builtin_amdgcn_raw_buffer_load_b32(row_rsrc(a.values + at, bytes), tid * 4, 0, kAuxKeep));
   };
   auto unpack = [&](const auto& v, float (&x)[E]) {
 #pragma unroll
@@ -171,6 +207,8 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
   };
   int64_t row = blockIdx.x;
   bool valid = row < a.T && is_valid(row);
+  load_entry(row, valid);
+  load_ahead(row, valid);
   load_row(row, valid);
   __syncthreads();                         // the lists are empty
   int parity = 0;                          // flips after each row that was evaluated
@@ -185,19 +223,32 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
     const int ei = sp.template entry<E>(tid);
     Record<NT>& rec = recs[parity];
     bool good = valid;
-    float tv = -INFINITY, tz = -INFINITY;  // this thread's entry of the record: value, student's logit
+    // This thread's entry of the record: id, value, the student's logit; and its single entry of the row.
+    int id = id_next;
+    const bool bad = valid && tid < a.k && (id < -1 || id >= V);
+    const bool holds = valid && tid < a.k && id >= 0 && !bad;
+    const float tv = holds ? tv_next : -INFINITY;
+    if constexpr (PF > 0) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int c = 0; c < PF; ++c) {
+        const u32x4 v = ahead[c * NT + tid];
+        r[c][0] = v.x;
+        r[c][1] = v.y;
+        r[c][2] = v.z;
+        r[c][3] = v.w;
+      }
+    }
+    // without branches, and used only behind the first pass: a load that misses its row's range reads 0
+    const __amdgpu_buffer_rsrc_t re = row_rsrc(zrow, V * (int)sizeof(Tin));
+    const uint32_t tz_word = load_one(re, holds ? id : -1), xe_word = load_one(re, valid && edge ? ei : -1);
+    load_entry(next, next_valid);
     if (valid) {
       // thread j holds entry j and hands it to the thread that owns its token
-      bool bad = false;
       if (tid < a.k) {
-        int id = a.tokens[row * a.k + tid];
-        bad = id < -1 || id >= V;
-        id = bad ? -1 : id;
-        rec.id[tid] = id;
+        rec.id[tid] = holds ? id : -1;
         rec.again[tid] = 0;
-        if (id >= 0) {
-          tv = a.values[row * a.k + tid];
-          tz = sizeof(Tin) == 2 ? bf16_to_f32(((const uint16_t*)zrow)[id]) : ((const float*)zrow)[id];
+        if (holds) {
           const int e = id - sp.lead;
           const int owner = e >= 0 && e < nfull * E ? (e / E) % NT : (e < 0 ? id : id - nfull * E);
           rec.next[tid] = (int16_t)atomicExch(&rec.head[owner], tid);
@@ -207,18 +258,29 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
       good = !__syncthreads_or(bad);       // a token outside the vocabulary makes the row bad
       parity ^= 1;
     }
+    int head = -1;
+    uint32_t slots = 0;                    // bit s mod 32: a record's token lies in chunk slot s
+    bool edge_held = false;
+    float xe = -INFINITY;                  // this thread's single entry
+    // the record's entries of this thread's chunk of a slot: f(j, entry of the chunk). What depends
+    // on the slot is uniform here and below: a value per slot and thread would be kept in a
+    // register across the rows.
+    auto held = [&](int slot, auto&& f) {
+      for (int j = head; j >= 0; j = rec.next[j]) {
+        const int e = rec.id[j] - (sp.lead + slot * NT * E) - tid * E;
+        if (e >= 0 && e < E) f(j, e);
+      }
+    };
+    const __amdgpu_buffer_rsrc_t rz = row_rsrc(zrow + sp.lead, nfull * 16);
     if (!good) {                           // uniform
       if (valid) rec.head[tid] = -1;
-      if (drow) zero_row<Tin, NT>(drow, V);
       if (tid == 0) {
         a.loss_tok[row] = 0.0f;
         a.flags[row] = valid ? (uint8_t)(DPPO_FLAG_VALID | DPPO_FLAG_BAD_ID) : (uint8_t)0;
       }
     } else {
-      const int head = rec.head[tid];
+      head = rec.head[tid];
       rec.head[tid] = -1;                  // the list stays reachable through `head`
-      uint32_t slots = 0;                  // bit s mod 32: a record's token lies in chunk slot s
-      bool edge_held = false;
       for (int j = head; j >= 0; j = rec.next[j]) {
         const int e = rec.id[j] - sp.lead;
         if (e >= 0 && e < nfull * E) slots |= 1u << ((e / E / NT) & 31);
@@ -229,15 +291,6 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
             rm.any_again = 1;
           }
       }
-      // the record's entries of this thread's chunk of a slot: f(j, entry of the chunk). What depends
-      // on the slot is uniform here and below: a value per slot and thread would be kept in a
-      // register across the rows.
-      auto held = [&](int slot, auto&& f) {
-        for (int j = head; j >= 0; j = rec.next[j]) {
-          const int e = rec.id[j] - (sp.lead + slot * NT * E) - tid * E;
-          if (e >= 0 && e < E) f(j, e);
-        }
-      };
       float N = kNoShift, S = 0.0f;
       auto add = [&](float (&x)[E], int slot) {
         if (slots >> (slot & 31) & 1u)
@@ -250,7 +303,6 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
         else cm = fmaxf(cm, x[3]);
         add_logits(N, S, x, cm, L);
       };
-      const __amdgpu_buffer_rsrc_t rz = row_rsrc(zrow + sp.lead, nfull * 16);
       // the chunks past the registers
       if constexpr (KS > 0) {
         for (int s0 = NC; s0 * NT < nfull; s0 += U) {
@@ -278,9 +330,8 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
         asm volatile("" : "+v"(r[c][0]), "+v"(r[c][1]), "+v"(r[c][2]), "+v"(r[c][3]));
         __builtin_amdgcn_sched_barrier(0);
       }
-      float xe = -INFINITY;
+      xe = value_of(xe_word);
       if (edge) {
-        xe = sizeof(Tin) == 2 ? bf16_to_f32(((const uint16_t*)zrow)[ei]) : ((const float*)zrow)[ei];
         bool own = false;
         if (edge_held)
           for (int j = head; j >= 0; j = rec.next[j]) own |= rec.id[j] == ei;
@@ -289,14 +340,19 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
       }
       if (tid < a.k) {
         rm.value[tid] = tv;
-        rm.z[tid] = tz;
+        rm.z[tid] = holds ? value_of(tz_word) : -INFINITY;
       }
       N = shift_of(N);
       block_merge_ns_int<NT>(N, S, red[parity]);
       if (tid < 64) record_math(a, row, scale * (a.tscale ? uload(a.tscale + row) : 1.0f), N, S, rec, rm);
       if (tid == 0) a.flags[row] = (uint8_t)DPPO_FLAG_VALID;
-      if (drow) {
-        __syncthreads();
+      __syncthreads();
+    }
+    load_ahead(next, next_valid);
+    if (!good) {
+      if (drow) zero_row<Tin, NT>(drow, V);
+    } else if (drow) {
+      {
         const float w = rm.w, l2 = rm.lse2;
         const __amdgpu_buffer_rsrc_t rd = row_rsrc(drow + sp.lead, nfull * 16);
         const bool same = (((uintptr_t)drow - (uintptr_t)zrow) & 15) == 0;    // uniform
@@ -374,17 +430,19 @@ struct Shape {
   int nt, nc;
   const void *bf16, *f32;
 };
-template <int NT, int NC, int KS>
+template <int NT, int NC, int KS, int PF>
 constexpr Shape shape() {
-  return {NT, NC, (const void*)distill_rows<uint16_t, NT, NC, KS>, (const void*)distill_rows<float, NT, NC, KS>};
+  return {NT, NC, (const void*)distill_rows<uint16_t, NT, NC, KS, PF>,
+          (const void*)distill_rows<float, NT, NC, KS, PF>};
 }
 
 }  // namespace
 
 hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
   // by the chunks of a row; the last takes rows of any length
-  static const Shape shapes[] = {shape<256, 2, 0>(), shape<256, 4, 0>(),   shape<256, 8, 0>(),   shape<512, 8, 0>(),
-                                 shape<1024, 8, 0>(), shape<1024, 12, 0>(), shape<1024, 19, 0>(), shape<1024, 16, 7>()};
+  static const Shape shapes[] = {shape<256, 2, 0, 0>(),  shape<256, 4, 0, 0>(),   shape<256, 8, 0, 0>(),
+                                 shape<512, 8, 0, 8>(),  shape<1024, 8, 0, 8>(),  shape<1024, 13, 0, 8>(),
+                                 shape<1024, 19, 0, 8>(), shape<1024, 16, 7, 0>()};
   const int64_t chunks = (int64_t)a.V * (bf16 ? 2 : 4) / 16;
   const Shape* s = shapes;
   while (s + 1 < shapes + sizeof(shapes) / sizeof(shapes[0]) && (int64_t)s->nt * s->nc < chunks) ++s;
