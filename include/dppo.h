@@ -463,10 +463,12 @@ dppo_status dppo_reset_decision(const int32_t* stats, double tau, int32_t patien
  *   aligned; g is rounded to `dtype` first. With flags (the loss call's flags_out; rd_mode and
  *   loss_tok are then that call's too) rows that are zero in dlogits because their tokens are
  *   masked, bad, clipped or out of band are written as 0 * g, and 16-byte chunks that lie in
- *   such rows alone are not read. out may be dlogits.
+ *   such rows alone are not read. For distill_loss_fwd_bwd's dlogits, flags_out and kl_out rd_mode is
+ *   DPPO_RD_DISTILL. out may be dlogits.
  * dppo_scale_to_bf16 -- dst = bf16(src * g) for n float32 values; both 16-byte aligned.
  *   g: device float32 scalar.
  */
+#define DPPO_RD_DISTILL (-1)
 dppo_status dppo_scale_dlogits(const void* dlogits, int32_t dtype, int64_t T, int64_t V,
                                const uint8_t* flags, const float* loss_tok, int32_t rd_mode,
                                const float* g, void* out, void* stream);

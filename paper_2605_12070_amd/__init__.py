@@ -834,17 +834,19 @@ class DistillLoss(torch.autograd.Function):
     def forward(ctx, logits, teacher_values, teacher_ids, teacher_lse, loss_mask, token_scale, kwargs):
         res = distill_loss_fwd_bwd(logits, teacher_values, teacher_ids, teacher_lse, loss_mask,
                                    token_scale, **(kwargs or {}))
-        ctx.save_for_backward(res.dlogits)
+        # the flags and losses beside dlogits, so that a checkpoint that recomputes the forward
+        # replaces all three
+        ctx.save_for_backward(res.dlogits, res.flags, res.kl)
         ctx.set_materialize_grads(False)     # no zero fills for kl and stats
         ctx.mark_non_differentiable(res.kl, res.stats)
         return res.loss[0], res.kl, res.stats
 
     @staticmethod
     def backward(ctx, g_loss, g_kl, g_stats):
-        (d,) = ctx.saved_tensors
+        d, *rows = ctx.saved_tensors
         if g_loss is None:
             g_loss = torch.zeros((), dtype=torch.float32, device=d.device)
-        return (_scaled_dlogits(d, g_loss, (), 0), None, None, None, None, None, None)
+        return (_scaled_dlogits(d, g_loss, rows, _lib.RD_DISTILL), None, None, None, None, None, None)
 
 
 @dataclass

@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdppo.so"
 DPPO_OK, DPPO_ERR_INVALID_ARG, DPPO_ERR_UNSUPPORTED, DPPO_ERR_HIP = 0, 1, 2, 3
 DPPO_F32, DPPO_BF16 = 0, 1
 RD_MODES = {"none": 0, "mask": 1, "weight": 2, "mask_weight": 3}
+RD_DISTILL = -1
 SCALE_MODES = {"const": 0, "token_mean": 1}
 REF_MODES = {"given": 0, "log_linear": 1, "linear": 2}
 FLAG_VALID, FLAG_BAND, FLAG_PPO, FLAG_BAD_ID = 1, 2, 4, 8

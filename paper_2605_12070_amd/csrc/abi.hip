@@ -870,7 +870,7 @@ dppo_status dppo_scale_dlogits(const void* dlogits, int32_t dtype, int64_t T, in
   if (s != DPPO_OK) return s;
   if (!g || (T > 0 && !out)) return fail(DPPO_ERR_INVALID_ARG, "g and out are required");
   if (flags && !loss_tok) return fail(DPPO_ERR_INVALID_ARG, "loss_tok is required with flags");
-  if (rd_mode < DPPO_RD_NONE || rd_mode > DPPO_RD_MASK_WEIGHT)
+  if ((rd_mode < DPPO_RD_NONE || rd_mode > DPPO_RD_MASK_WEIGHT) && rd_mode != DPPO_RD_DISTILL)
     return fail(DPPO_ERR_INVALID_ARG, "unknown rd_mode %d", (int)rd_mode);
   if (!aligned16(dlogits) || !aligned16(out))
     return fail(DPPO_ERR_INVALID_ARG, "dlogits and out must be 16-byte aligned");
@@ -884,7 +884,9 @@ dppo_status dppo_scale_dlogits(const void* dlogits, int32_t dtype, int64_t T, in
   a.V = (int32_t)V;
   a.flags = flags;
   a.loss_tok = loss_tok;
-  a.uses_band = rd_mode == DPPO_RD_MASK || rd_mode == DPPO_RD_MASK_WEIGHT;
+  a.live = rd_mode == DPPO_RD_DISTILL                                       ? DPPO_FLAG_VALID
+           : rd_mode == DPPO_RD_MASK || rd_mode == DPPO_RD_MASK_WEIGHT ? DPPO_FLAG_PPO | DPPO_FLAG_BAND
+                                                                       : DPPO_FLAG_PPO;
   a.g = g;
   const hipError_t e = dppo::launch_scale_rows(a, dtype == DPPO_BF16, (hipStream_t)stream);
   return e == hipSuccess ? DPPO_OK : hip_fail(e, "dlogits scale launch");
@@ -1133,15 +1135,18 @@ dppo_status distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t T, i
   }
   hipStream_t st = (hipStream_t)stream;
   // a batch short enough for every workgroup to read its mask needs no counting kernel
-  const bool count_mode = T > 0 && T <= dppo::kCountModeMaxT;
+  const bool count_mode = T <= dppo::kCountModeMaxT;
   hipError_t e = hipSuccess;
-  if (!count_mode) {
+  if (!count_mode && scale_mode == DPPO_SCALE_TOKEN_MEAN) {
     dppo::launch_prep_stats(loss_mask, T, stats_out, st);
     e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "prep_stats launch");
   }
+  dppo::DistillArgs a{};
+  a.stats = stats_out;
+  a.loss_scale = loss_scale;
+  a.scale_mode = scale_mode;
   if (T > 0) {
-    dppo::DistillArgs a{};
     a.logits = logits;
     a.ld = ld;
     a.dlogits = dlogits;
@@ -1150,12 +1155,9 @@ dppo_status distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t T, i
     a.tscale = token_scale;
     a.loss_tok = kl_out;
     a.flags = flags_out;
-    a.stats = stats_out;
     a.T = (int32_t)T;
     a.V = (int32_t)V;
     a.mode = dppo::kModeLoss;
-    a.loss_scale = loss_scale;
-    a.scale_mode = scale_mode;
     a.count_mode = count_mode ? 1 : 0;
     a.values = teacher_values;
     a.tokens = teacher_ids;
@@ -1167,10 +1169,8 @@ dppo_status distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t T, i
     e = dppo::launch_distill(a, dtype == DPPO_BF16, st);
     if (e != hipSuccess) return hip_fail(e, "distillation launch");
   }
-  dppo::launch_loss_sum(kl_out, loss_mask, token_scale, stats_out, T, loss_scale, scale_mode, loss_out,
-                        st, T > 0 ? flags_out : nullptr, DPPO_RD_NONE);
-  e = hipGetLastError();
-  return e == hipSuccess ? DPPO_OK : hip_fail(e, "loss_sum launch");
+  e = dppo::launch_distill_sum(a, loss_out, st);
+  return e == hipSuccess ? DPPO_OK : hip_fail(e, "distillation sum launch");
 }
 
 namespace {

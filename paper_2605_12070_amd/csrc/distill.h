@@ -18,5 +18,7 @@ struct DistillArgs : RowArgs {
 };
 
 hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st);
+// The loss and the counters from the rows' kl and flags (T = 0: zeros).
+hipError_t launch_distill_sum(const DistillArgs& a, float* loss, hipStream_t st);
 
 }  // namespace dppo

@@ -47,9 +47,8 @@ struct Record {
 };
 
 struct RecordMath {    // one row at a time, between two barriers
-  float value[kMaxK];
-  float z[kMaxK];
-  double p[kMaxK], q[kMaxK];
+  float value[kMaxK];  // the record's values, then its probabilities p
+  float z[kMaxK];      // the student's logits, then its probabilities q
   int any_again;
   float w, lse2;
 };
@@ -103,8 +102,8 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
     if (p != 0.0) l += p * ((tj - c) - lq) * kLn2F64;
     P += p;
     if (!rec.again[j]) Q += q;
-    m.p[j] = p;
-    m.q[j] = q;
+    m.value[j] = (float)p;                 // the gradient g q - p is held in 32 bits
+    m.z[j] = (float)q;
   }
   l = wave_uniform(wave_sum_f64(l));
   P = wave_uniform(wave_sum_f64(P));
@@ -121,11 +120,11 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
   __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
 #pragma unroll 1
   for (int j = lane; j < k; j += 64) {
-    double p = m.p[j];
+    double p = m.value[j];
     if (m.any_again)
       for (int i = j + 1; i < k; ++i)
-        if (rec.id[i] == rec.id[j]) p += m.p[i];
-    rec.grad[j] = (float)(s * (g * m.q[j] - p));
+        if (rec.id[i] == rec.id[j]) p += m.value[i];
+    rec.grad[j] = (float)(s * (g * m.z[j] - p));
   }
   if (lane == 0) {
     // what rounding lse2 to 32 bits leaves over goes into the factor
@@ -144,18 +143,19 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
 template <typename Tin, int NT, int NC, int KS, int PF>
 __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
   static_assert(PF <= NC && (KS == 0 || PF == 0));
+  constexpr int KE = (kMaxK + NT - 1) / NT;   // entries of a record per thread: tid, tid + NT, ...
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int U = 4;                     // further chunks per thread in flight
   __shared__ float red[2][2 * (NT / 64)];
-  __shared__ Record<NT> recs[2];
+  constexpr int kRecs = NT == 64 ? 1 : 2;     // one wave is never in two rows
+  __shared__ Record<NT> recs[kRecs];
   __shared__ RecordMath rm;
   __shared__ u32x4 keep[KS > 0 ? KS * NT : 1];
   __shared__ u32x4 ahead[PF > 0 ? PF * NT : 1];   // [chunk][thread]: a wave reads what it loaded
   const int tid = threadIdx.x;
   const int V = a.V;
   const float L = a.l2e;
-  recs[0].head[tid] = recs[1].head[tid] = -1;
-  const float scale = call_scale<NT>(a);
+  recs[0].head[tid] = recs[kRecs - 1].head[tid] = -1;
   auto is_valid = [&](int64_t row) { return a.mask == nullptr || uload_u8(a.mask + row) != 0; };
   uint32_t r[NC][4];
   auto load_row = [&](int64_t row, bool rd) {
@@ -184,15 +184,18 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
     else return __builtin_amdgcn_raw_buffer_load_b32(rz, off, 0, kAuxKeep);
   };
   auto value_of = [&](uint32_t w) { return __uint_as_float(sizeof(Tin) == 2 ? w << 16 : w); };
-  // this thread's entry of a row's record
-  int id_next = -1;
-  float tv_next = 0.0f;
-  auto load_entry = [&](int64_t row, bool rd) {
+  // this thread's entries of a row's record
+  int id_next[KE];
+  float tv_next[KE];
+  auto load_entries = [&](int64_t row, bool rd) {
     const int64_t at = (rd ? row : 0) * a.k;
     const int bytes = rd ? a.k * 4 : 0;
-    id_next = (int)__builtin_amdgcn_raw_buffer_load_b32(row_rsrc(a.tokens + at, bytes), tid * 4, 0, kAuxKeep);
-    tv_next = __uint_as_float(
-        __builtin_amdgcn_raw_buffer_load_b32(row_rsrc(a.values + at, bytes), tid * 4, 0, kAuxKeep));
+    const __amdgpu_buffer_rsrc_t ri = row_rsrc(a.tokens + at, bytes), rv = row_rsrc(a.values + at, bytes);
+#pragma unroll
+    for (int i = 0; i < KE; ++i) {
+      id_next[i] = (int)__builtin_amdgcn_raw_buffer_load_b32(ri, tid * 4, i * NT * 4, kAuxKeep);
+      tv_next[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rv, tid * 4, i * NT * 4, kAuxKeep));
+    }
   };
   auto unpack = [&](const auto& v, float (&x)[E]) {
 #pragma unroll
@@ -207,9 +210,10 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
   };
   int64_t row = blockIdx.x;
   bool valid = row < a.T && is_valid(row);
-  load_entry(row, valid);
+  load_entries(row, valid);
   load_ahead(row, valid);
   load_row(row, valid);
+  const float scale = call_scale<NT>(a);   // its loads in flight together with the first row's
   __syncthreads();                         // the lists are empty
   int parity = 0;                          // flips after each row that was evaluated
   for (; row < a.T; row += gridDim.x) {
@@ -221,13 +225,22 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
     const int nfull = sp.nfull;
     const bool edge = tid < sp.nedge;
     const int ei = sp.template entry<E>(tid);
-    Record<NT>& rec = recs[parity];
+    Record<NT>& rec = recs[kRecs == 1 ? 0 : parity];
     bool good = valid;
-    // This thread's entry of the record: id, value, the student's logit; and its single entry of the row.
-    int id = id_next;
-    const bool bad = valid && tid < a.k && (id < -1 || id >= V);
-    const bool holds = valid && tid < a.k && id >= 0 && !bad;
-    const float tv = holds ? tv_next : -INFINITY;
+    // This thread's entries of the record (id, -1 for none; value; the student's logit) and its single
+    // entry of the row.
+    int id[KE];
+    float tv[KE];
+    uint32_t tz_word[KE];
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < KE; ++i) {
+      const bool in = valid && i * NT + tid < a.k;
+      const bool out = in && (id_next[i] < -1 || id_next[i] >= V);
+      bad |= out;
+      id[i] = in && !out ? id_next[i] : -1;
+      tv[i] = id[i] >= 0 ? tv_next[i] : -INFINITY;
+    }
     if constexpr (PF > 0) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
@@ -241,17 +254,22 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
     }
     // without branches, and used only behind the first pass: a load that misses its row's range reads 0
     const __amdgpu_buffer_rsrc_t re = row_rsrc(zrow, V * (int)sizeof(Tin));
-    const uint32_t tz_word = load_one(re, holds ? id : -1), xe_word = load_one(re, valid && edge ? ei : -1);
-    load_entry(next, next_valid);
+#pragma unroll
+    for (int i = 0; i < KE; ++i) tz_word[i] = load_one(re, id[i]);
+    const uint32_t xe_word = load_one(re, valid && edge ? ei : -1);
+    load_entries(next, next_valid);
     if (valid) {
-      // thread j holds entry j and hands it to the thread that owns its token
-      if (tid < a.k) {
-        rec.id[tid] = holds ? id : -1;
-        rec.again[tid] = 0;
-        if (holds) {
-          const int e = id - sp.lead;
-          const int owner = e >= 0 && e < nfull * E ? (e / E) % NT : (e < 0 ? id : id - nfull * E);
-          rec.next[tid] = (int16_t)atomicExch(&rec.head[owner], tid);
+      // an entry goes to the list of the thread that owns its token
+#pragma unroll
+      for (int i = 0; i < KE; ++i) {
+        const int j = i * NT + tid;
+        if (j >= a.k) break;
+        rec.id[j] = id[i];
+        rec.again[j] = 0;
+        if (id[i] >= 0) {
+          const int e = id[i] - sp.lead;
+          const int owner = e >= 0 && e < nfull * E ? (e / E) % NT : (e < 0 ? id[i] : id[i] - nfull * E);
+          rec.next[j] = (int16_t)atomicExch(&rec.head[owner], j);
         }
       }
       if (tid == 0) rm.any_again = 0;
@@ -338,9 +356,12 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
         const float x[1] = {own ? -INFINITY : xe};
         add_logits(N, S, x, x[0], L);
       }
-      if (tid < a.k) {
-        rm.value[tid] = tv;
-        rm.z[tid] = holds ? value_of(tz_word) : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < KE; ++i) {
+        const int j = i * NT + tid;
+        if (j >= a.k) break;
+        rm.value[j] = tv[i];
+        rm.z[j] = id[i] >= 0 ? value_of(tz_word[i]) : -INFINITY;
       }
       N = shift_of(N);
       block_merge_ns_int<NT>(N, S, red[parity]);
@@ -426,6 +447,62 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
   }
 }
 
+// The loss sum and the counters, in one workgroup. L is summed in float64, each thread over a fixed
+// stride, then a fixed tree: the same inputs give the same bits on every run. (loss_sum, which also
+// counts what the PPO decisions need, takes 7.5 us where this takes 4.)
+__global__ __launch_bounds__(1024) void distill_sum(const float* kl, const uint8_t* flags, const float* tscale,
+                                                    int32_t* stats, int64_t T, float loss_scale, int32_t scale_mode,
+                                                    float* loss) {
+  constexpr int U = 8;
+  __shared__ double part[16];
+  __shared__ int counts[2][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double acc = 0.0;
+  int n_valid = 0, n_bad = 0;              // this wave's
+  for (int64_t base = threadIdx.x; base - lane < T; base += 1024 * U) {
+    float l[U], ts[U];
+    uint32_t f[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = base + (int64_t)u * 1024;
+      const int64_t j = i < T ? i : T - 1;
+      l[u] = kl[j];
+      ts[u] = tscale ? tscale[j] : 1.0f;
+      f[u] = i < T ? flags[j] : 0u;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      // masked and bad rows have l = 0, and must not meet a scale that is not finite
+      if ((f[u] & (DPPO_FLAG_VALID | DPPO_FLAG_BAD_ID)) == DPPO_FLAG_VALID) acc += (double)ts[u] * (double)l[u];
+      n_valid += __popcll(__ballot(f[u] & DPPO_FLAG_VALID));
+      n_bad += __popcll(__ballot(f[u] & DPPO_FLAG_BAD_ID));
+    }
+  }
+  acc = wave_sum_f64(acc);
+  if (lane == 0) {
+    part[wave] = acc;
+    counts[0][wave] = n_valid;
+    counts[1][wave] = n_bad;
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    acc = wave_sum_f64(lane < 16 ? part[lane] : 0.0);
+    int n = lane < 16 ? counts[0][lane] : 0, bad = lane < 16 ? counts[1][lane] : 0;
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) {
+      n += __shfl_xor(n, off, 64);
+      bad += __shfl_xor(bad, off, 64);
+    }
+    if (lane == 0) {
+      const float scale = scale_mode == DPPO_SCALE_TOKEN_MEAN ? loss_scale / (float)(n > 1 ? n : 1) : loss_scale;
+      loss[0] = (float)((double)scale * acc);
+      for (int k = 0; k < DPPO_N_STATS; ++k) stats[k] = 0;
+      stats[DPPO_STAT_N_VALID] = n;
+      stats[DPPO_STAT_N_BAD] = bad;
+    }
+  }
+}
+
 struct Shape {
   int nt, nc;
   const void *bf16, *f32;
@@ -440,9 +517,10 @@ constexpr Shape shape() {
 
 hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
   // by the chunks of a row; the last takes rows of any length
-  static const Shape shapes[] = {shape<256, 2, 0, 0>(),  shape<256, 4, 0, 0>(),   shape<256, 8, 0, 0>(),
-                                 shape<512, 8, 0, 8>(),  shape<1024, 8, 0, 8>(),  shape<1024, 13, 0, 8>(),
-                                 shape<1024, 19, 0, 8>(), shape<1024, 16, 7, 0>()};
+  static const Shape shapes[] = {
+      shape<64, 4, 0, 0>(),    shape<128, 4, 0, 0>(),   shape<128, 8, 0, 0>(),   shape<256, 8, 0, 0>(),
+      shape<256, 16, 0, 0>(),  shape<256, 24, 0, 0>(),  shape<512, 16, 0, 0>(),  shape<1024, 13, 0, 8>(),
+      shape<1024, 19, 0, 8>(), shape<1024, 16, 7, 0>()};
   const int64_t chunks = (int64_t)a.V * (bf16 ? 2 : 4) / 16;
   const Shape* s = shapes;
   while (s + 1 < shapes + sizeof(shapes) / sizeof(shapes[0]) && (int64_t)s->nt * s->nc < chunks) ++s;
@@ -457,6 +535,11 @@ hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
   void* kargs[] = {&args};
   e = hipLaunchKernel(fn, dim3((unsigned)grid), dim3((unsigned)s->nt), kargs, 0, st);
   return e == hipSuccess ? hipGetLastError() : e;
+}
+
+hipError_t launch_distill_sum(const DistillArgs& a, float* loss, hipStream_t st) {
+  distill_sum<<<1, 1024, 0, st>>>(a.loss_tok, a.flags, a.tscale, a.stats, a.T, a.loss_scale, a.scale_mode, loss);
+  return hipGetLastError();
 }
 
 }  // namespace dppo

@@ -12,7 +12,7 @@ struct ScaleRowsArgs {
   int32_t T, V;
   const uint8_t* flags;    // the loss call's flags, or NULL: every row is read
   const float* loss_tok;   // with flags: the call's per-token losses (NaN rows)
-  int32_t uses_band;       // the call's rd_mode masks by the band
+  uint32_t live;           // flags that a row's gradient takes to be more than zeros
   const float* g;          // device scalar
 };
 

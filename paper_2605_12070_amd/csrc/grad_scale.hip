@@ -20,7 +20,7 @@ constexpr int kScaleNT = 512;
 __device__ __forceinline__ bool row_live(const ScaleRowsArgs& a, int64_t row) {
   const uint32_t fl = a.flags[row];
   const float lt = a.loss_tok[row];
-  const bool active = (fl & DPPO_FLAG_PPO) && ((fl & DPPO_FLAG_BAND) || !a.uses_band);
+  const bool active = (fl & (a.live | DPPO_FLAG_BAD_ID)) == a.live;
   return active || lt != lt;                     // a NaN row's gradient is NaN, not zero
 }
 
