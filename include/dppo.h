@@ -538,6 +538,30 @@ dppo_status distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t T, i
                                  int32_t* stats_out, void* dlogits, int64_t ld_dlogits, void* stream);
 
 /*
+ * distill_loss_call -- distill_loss_fwd_bwd with its arguments in one struct (the same meaning and
+ * checks), as decoupled_ppo_loss_call.
+ */
+typedef struct dppo_distill_call {
+  const void* logits;
+  int64_t dtype, T, V, ld;
+  const float* teacher_values;
+  const int32_t* teacher_ids;
+  int64_t k;
+  const float* teacher_lse;
+  const uint8_t* loss_mask;
+  const float* token_scale;
+  float *kl_out, *loss_out;
+  uint8_t* flags_out;
+  int32_t* stats_out;
+  void* dlogits;
+  int64_t ld_dlogits;
+  void* stream;
+  int64_t scale_mode;
+  double temperature, loss_scale;
+} dppo_distill_call;
+dppo_status distill_loss_call(const dppo_distill_call* call);
+
+/*
  * verify_drafts -- speculative decoding's check of drafted tokens against the policy, with the
  * caller's random numbers, so that the emitted tokens are distributed as the policy's own samples.
  * For sequence b with n = num_drafts[b] drafts x_0 .. x_{n-1}, p_i = softmax(target[b, i] / tau),
@@ -570,6 +594,24 @@ dppo_status verify_drafts(const void* target, int64_t target_seq, int64_t target
                           const float* accept_u, const float* sample_u, double temperature,
                           int32_t* accepted_out, int64_t* tokens_out, float* logp_out, void* workspace,
                           int64_t workspace_bytes, void* stream);
+/* The same with its arguments in one struct, as decoupled_ppo_loss_call. */
+typedef struct dppo_verify_call {
+  const void* target;
+  int64_t target_seq, target_row;
+  const void* draft;
+  int64_t draft_seq, draft_row, dtype, B, D, V;
+  const int64_t* draft_ids;
+  const int32_t* num_drafts;
+  const float *accept_u, *sample_u;
+  int32_t* accepted_out;
+  int64_t* tokens_out;
+  float* logp_out;
+  void* workspace;
+  int64_t workspace_bytes;
+  void* stream;
+  double temperature;
+} dppo_verify_call;
+dppo_status verify_drafts_call(const dppo_verify_call* call);
 /* Workspace bytes of such a call (-1 if the sizes are out of range). with_draft: draft is given. */
 int64_t verify_drafts_workspace_bytes(int32_t dtype, int64_t B, int64_t D, int64_t V, int32_t with_draft);
 

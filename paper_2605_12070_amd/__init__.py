@@ -722,27 +722,19 @@ def _plain(t: torch.Tensor, name: str):
 
 
 def _tensor(t, shape, dtype, name, dev):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not _plain(t, name).is_contiguous():
+    if t.dtype != dtype or t.shape != shape or t.is_neg() or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {list(shape)} {dtype} tensor")
     if t.device != dev:
         raise ValueError(f"{name} must live on {dev}")
     return t.data_ptr()
 
 
-class _on_device:
-    """The tensors' device as the current one while a call launches on it."""
-
-    def __init__(self, dev):
-        self.want = dev.index
-
-    def __enter__(self):
-        self.old = torch._C._cuda_getDevice()
-        if self.old != self.want:
-            torch.cuda.set_device(self.want)
-
-    def __exit__(self, *exc):
-        if self.old != self.want:
-            torch.cuda.set_device(self.old)
+def _launch(dev, call, *args):
+    """A library call with the tensors' device as the current one."""
+    if torch._C._cuda_getDevice() == dev.index:
+        return call(*args)
+    with torch.cuda.device(dev):
+        return call(*args)
 
 
 @dataclass
@@ -766,10 +758,9 @@ def top_logits(logits: torch.Tensor, k: int, *, temperature: float = 1.0) -> Top
     ids = torch.empty(T, rows, dtype=torch.int32, device=dev)
     lse = torch.empty(T, dtype=torch.float32, device=dev)
     ws = torch.empty(n, dtype=torch.uint8, device=dev) if n > 0 else None
-    with _on_device(dev):
-        st = _lib.lib().top_logits(ptr, code, T, V, ld, k, float(temperature), values.data_ptr(),
-                                   ids.data_ptr(), lse.data_ptr(),
-                                   ws.data_ptr() if ws is not None else None, max(n, 0), _stream(dev))
+    st = _launch(dev, _lib.lib().top_logits, ptr, code, T, V, ld, k, float(temperature), values.data_ptr(),
+                 ids.data_ptr(), lse.data_ptr(), ws.data_ptr() if ws is not None else None, max(n, 0),
+                 _stream(dev))
     _lib.check(st, "top_logits")
     return TopLogits(values, ids, lse)
 
@@ -799,29 +790,30 @@ def distill_loss_fwd_bwd(logits, teacher_values, teacher_ids, teacher_lse=None, 
     k = teacher_values.shape[1]
     tv = _tensor(teacher_values, (T, k), torch.float32, "teacher_values", dev)
     ti = _tensor(teacher_ids, (T, k), torch.int32, "teacher_ids", dev)
-    tl = None if teacher_lse is None else _tensor(teacher_lse, (T,), torch.float32, "teacher_lse", dev)
+    tl = 0 if teacher_lse is None else _tensor(teacher_lse, (T,), torch.float32, "teacher_lse", dev)
     msk = _vec(loss_mask, T, torch.uint8, "loss_mask", dev, optional=True)
-    tsc = None if token_scale is None else _tensor(token_scale, (T,), torch.float32, "token_scale", dev)
+    tsc = 0 if token_scale is None else _tensor(token_scale, (T,), torch.float32, "token_scale", dev)
     if scale_mode not in SCALE_MODES:
         raise ValueError(f"scale_mode in {list(SCALE_MODES)}")
     f32 = dict(dtype=torch.float32, device=dev)
     out = DistillResult(loss=torch.empty(1, **f32), kl=torch.empty(T, **f32),
                         flags=torch.empty(T, dtype=torch.uint8, device=dev),
                         stats=torch.empty(_lib.N_STATS, dtype=torch.int32, device=dev), dlogits=None)
-    d_ptr, ldd = None, 0
+    d_ptr, ldd = 0, 0
     if want_dlogits:
         if dlogits is None:
             dlogits = torch.empty_like(logits)
-        if (dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.stride(1) != 1
-                or dlogits.device != dev):
+        elif (dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.device != dev
+                or (V > 1 and dlogits.stride(1) != 1) or dlogits.is_neg()):
             raise ValueError("dlogits must match logits in dtype, shape and device, unit last stride")
-        out.dlogits = _plain(dlogits, "dlogits")
+        out.dlogits = dlogits
         d_ptr, ldd = dlogits.data_ptr(), dlogits.stride(0)
-    with _on_device(dev):
-        st = _lib.lib().distill_loss_fwd_bwd(
-            ptr, _dtype_code(logits), T, V, ld, tv, ti, k, tl, msk, tsc, float(temperature),
-            SCALE_MODES[scale_mode], float(loss_scale), out.kl.data_ptr(), out.loss.data_ptr(),
-            out.flags.data_ptr(), out.stats.data_ptr(), d_ptr, ldd, _stream(dev))
+    # None pointers are 0; the order is dppo_distill_call's
+    call = _lib.DISTILL_CALL.pack(
+        ptr, _dtype_code(logits), T, V, ld, tv, ti, k, tl, msk or 0, tsc, out.kl.data_ptr(),
+        out.loss.data_ptr(), out.flags.data_ptr(), out.stats.data_ptr(), d_ptr, ldd, _stream(dev),
+        SCALE_MODES[scale_mode], temperature, loss_scale)
+    st = _launch(dev, _lib.lib().distill_loss_call, call)
     _lib.check(st, "distill_loss_fwd_bwd")
     return out
 
@@ -857,10 +849,10 @@ class VerifyResult:
 
 
 def _rows3(t, name, B, rows, V, dtype, dev):
-    if t.dtype != dtype or tuple(t.shape) != (B, rows, V) or t.device != dev or \
-            (V > 1 and _plain(t, name).stride(2) != 1):
+    stride = t.stride()
+    if t.dtype != dtype or t.shape != (B, rows, V) or t.device != dev or t.is_neg() or (V > 1 and stride[2] != 1):
         raise ValueError(f"{name} must be a [{B}, {rows}, {V}] {dtype} tensor on {dev} with unit last stride")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), stride[0], stride[1]
 
 
 def verify_drafts(target_logits, draft_ids, accept_u, sample_u, draft_logits=None, num_drafts=None, *,
@@ -880,21 +872,22 @@ def verify_drafts(target_logits, draft_ids, accept_u, sample_u, draft_logits=Non
     dev = target_logits.device
     code = _dtype_code(target_logits)
     t_ptr, t_seq, t_row = _rows3(target_logits, "target_logits", B, D1, V, target_logits.dtype, dev)
-    q_ptr, q_seq, q_row = (None, 0, 0) if draft_logits is None else \
+    q_ptr, q_seq, q_row = (0, 0, 0) if draft_logits is None else \
         _rows3(draft_logits, "draft_logits", B, D, V, target_logits.dtype, dev)
     ids = _tensor(draft_ids, (B, D), torch.int64, "draft_ids", dev)
     u = _tensor(accept_u, (B, D), torch.float32, "accept_u", dev)
     un = _tensor(sample_u, (B,), torch.float32, "sample_u", dev)
-    num = None if num_drafts is None else _tensor(num_drafts, (B,), torch.int32, "num_drafts", dev)
+    num = 0 if num_drafts is None else _tensor(num_drafts, (B,), torch.int32, "num_drafts", dev)
     n = _lib.lib().verify_drafts_workspace_bytes(code, B, D, V, int(draft_logits is not None and D > 0))
     out = VerifyResult(accepted=torch.empty(B, dtype=torch.int32, device=dev),
                        tokens=torch.empty(B, D1, dtype=torch.int64, device=dev),
                        logp=torch.empty(B, D1, dtype=torch.float32, device=dev))
     ws = torch.empty(n, dtype=torch.uint8, device=dev) if n > 0 else None
-    with _on_device(dev):
-        st = _lib.lib().verify_drafts(
-            t_ptr, t_seq, t_row, q_ptr, q_seq, q_row, code, B, D, V, ids, num, u, un,
-            float(temperature), out.accepted.data_ptr(), out.tokens.data_ptr(), out.logp.data_ptr(),
-            ws.data_ptr() if ws is not None else None, max(n, 0), _stream(dev))
+    # the order is dppo_verify_call's
+    call = _lib.VERIFY_CALL.pack(
+        t_ptr, t_seq, t_row, q_ptr, q_seq, q_row, code, B, D, V, ids, num, u, un,
+        out.accepted.data_ptr(), out.tokens.data_ptr(), out.logp.data_ptr(),
+        ws.data_ptr() if ws is not None else 0, max(n, 0), _stream(dev), temperature)
+    st = _launch(dev, _lib.lib().verify_drafts_call, call)
     _lib.check(st, "verify_drafts")
     return out

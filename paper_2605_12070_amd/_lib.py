@@ -48,6 +48,11 @@ class DppoEwmaState(C.Structure):
 LOSS_CALL = struct.Struct("=19q4f2ifif4x")
 
 
+# dppo_distill_call and dppo_verify_call: pointers and 64-bit integers, then doubles.
+DISTILL_CALL = struct.Struct("=19q2d")
+VERIFY_CALL = struct.Struct("=20qd")
+
+
 def pack_loss_call(*fields) -> bytes:
     """A dppo_loss_call (fields in order, None for a NULL pointer already 0)."""
     try:
@@ -92,6 +97,8 @@ SIGNATURES = {
                                    VP, VP, VP, VP, VP, I64, VP]),
     "verify_drafts": (I32, [VP, I64, I64, VP, I64, I64, I32, I64, I64, I64, VP, VP, VP, VP, F64,
                             VP, VP, VP, VP, I64, VP]),
+    "distill_loss_call": (I32, [C.c_char_p]),
+    "verify_drafts_call": (I32, [C.c_char_p]),
     "verify_drafts_workspace_bytes": (I64, [I32, I64, I64, I64, I32]),
     "dppo_effective_thresholds": (I32, [C.c_double, C.c_double, C.c_double, C.c_double,
                                         C.c_double, I32, C.POINTER(C.c_double)]),

@@ -1237,4 +1237,28 @@ dppo_status verify_drafts(const void* target, int64_t target_seq, int64_t target
   return e == hipSuccess ? DPPO_OK : hip_fail(e, "draft verification launch");
 }
 
+dppo_status distill_loss_call(const dppo_distill_call* c) {
+  if (!c) return fail(DPPO_ERR_INVALID_ARG, "call pointer is NULL");
+  if (c->dtype != DPPO_F32 && c->dtype != DPPO_BF16)
+    return fail(DPPO_ERR_INVALID_ARG, "unknown dtype %lld", (long long)c->dtype);
+  if (c->k < 1 || c->k > DPPO_MAX_TOP)
+    return fail(DPPO_ERR_INVALID_ARG, "k = %lld out of [1, %d]", (long long)c->k, DPPO_MAX_TOP);
+  if (c->scale_mode != DPPO_SCALE_CONST && c->scale_mode != DPPO_SCALE_TOKEN_MEAN)
+    return fail(DPPO_ERR_INVALID_ARG, "unknown scale_mode %lld", (long long)c->scale_mode);
+  return distill_loss_fwd_bwd(c->logits, (int32_t)c->dtype, c->T, c->V, c->ld, c->teacher_values, c->teacher_ids,
+                              (int32_t)c->k, c->teacher_lse, c->loss_mask, c->token_scale, c->temperature,
+                              (int32_t)c->scale_mode, (float)c->loss_scale, c->kl_out, c->loss_out, c->flags_out,
+                              c->stats_out, c->dlogits, c->ld_dlogits, c->stream);
+}
+
+dppo_status verify_drafts_call(const dppo_verify_call* c) {
+  if (!c) return fail(DPPO_ERR_INVALID_ARG, "call pointer is NULL");
+  if (c->dtype != DPPO_F32 && c->dtype != DPPO_BF16)
+    return fail(DPPO_ERR_INVALID_ARG, "unknown dtype %lld", (long long)c->dtype);
+  return verify_drafts(c->target, c->target_seq, c->target_row, c->draft, c->draft_seq, c->draft_row,
+                       (int32_t)c->dtype, c->B, c->D, c->V, c->draft_ids, c->num_drafts, c->accept_u, c->sample_u,
+                       c->temperature, c->accepted_out, c->tokens_out, c->logp_out, c->workspace,
+                       c->workspace_bytes, c->stream);
+}
+
 }  // extern "C"

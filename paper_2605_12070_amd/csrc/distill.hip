@@ -21,6 +21,7 @@
 #include "distill.h"
 
 #include <algorithm>
+#include <mutex>
 
 #include "dppo_device.h"
 #include "f64_math.h"
@@ -515,6 +516,36 @@ constexpr Shape shape() {
 
 }  // namespace
 
+namespace {
+// Workgroups of a kernel that fit on the current device at once; the query takes microseconds, so it
+// is made once per device and kernel (more of them than the table holds are asked for each time).
+hipError_t resident_groups(const void* fn, int threads, int64_t* groups) {
+  struct Known {
+    int dev;
+    const void* fn;
+    int64_t groups;
+  };
+  static std::mutex mu;
+  static Known known[256];
+  static int count = 0;
+  int dev = 0, cus = 0, per_cu = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  std::lock_guard<std::mutex> lock(mu);
+  for (int i = 0; i < count; ++i)
+    if (known[i].dev == dev && known[i].fn == fn) {
+      *groups = known[i].groups;
+      return hipSuccess;
+    }
+  e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, fn, threads, 0);
+  if (e != hipSuccess) return e;
+  *groups = (int64_t)cus * std::max(per_cu, 1);
+  if (count < 256) known[count++] = {dev, fn, *groups};
+  return hipSuccess;
+}
+}  // namespace
+
 hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
   // by the chunks of a row; the last takes rows of any length
   static const Shape shapes[] = {
@@ -525,12 +556,10 @@ hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
   const Shape* s = shapes;
   while (s + 1 < shapes + sizeof(shapes) / sizeof(shapes[0]) && (int64_t)s->nt * s->nc < chunks) ++s;
   const void* fn = bf16 ? s->bf16 : s->f32;
-  int dev = 0, cus = 0, per_cu = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
-  if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, fn, s->nt, 0);
+  int64_t slots = 0;
+  hipError_t e = resident_groups(fn, s->nt, &slots);
   if (e != hipSuccess) return e;
-  const int64_t grid = std::min<int64_t>(a.T, (int64_t)cus * std::max(per_cu, 1));
+  const int64_t grid = std::min<int64_t>(a.T, slots);
   DistillArgs args = a;
   void* kargs[] = {&args};
   e = hipLaunchKernel(fn, dim3((unsigned)grid), dim3((unsigned)s->nt), kargs, 0, st);
