@@ -11,7 +11,7 @@
 // sure of the record's tokens. So the record's entries leave the sum of exponentials when their
 // chunk is read, and the record's own exponentials join it afterwards.
 //
-// A workgroup handles a row (persistent, looping over rows). The row's first NT NC 16-byte chunks
+// A workgroup handles a row (some shapes loop over rows). The row's first NT NC 16-byte chunks
 // stay in registers as they were read, the next KS NT in LDS, and only the rest of a longer row is
 // read again for the gradient. Every entry belongs to one thread (RowSplit; chunk c to thread
 // c mod NT), which finds the record's tokens among its entries in a list of its own (built in LDS by
@@ -504,13 +504,19 @@ __global__ __launch_bounds__(1024) void distill_sum(const float* kl, const uint8
   }
 }
 
+constexpr int64_t kMaxGrid = 1 << 20;      // HIP holds a grid's threads to 32 bits
+
 struct Shape {
   int nt, nc;
+  int rounds;          // workgroups per place on the device, 0: one per row
   const void *bf16, *f32;
 };
+// The loads ahead hide the record's arithmetic behind memory: with and without, us: bf16 k = 32, T = 4096,
+// V = 106495 412 and 426, V = 155647 602 and 614; fp32 k = 128, T = 4096, V = 50257 401 and 415, though
+// 377 and 371 at k = 32.
 template <int NT, int NC, int KS, int PF>
-constexpr Shape shape() {
-  return {NT, NC, (const void*)distill_rows<uint16_t, NT, NC, KS, PF>,
+constexpr Shape shape(int rounds) {
+  return {NT, NC, rounds, (const void*)distill_rows<uint16_t, NT, NC, KS, PF>,
           (const void*)distill_rows<float, NT, NC, KS, PF>};
 }
 
@@ -547,11 +553,19 @@ hipError_t resident_groups(const void* fn, int threads, int64_t* groups) {
 }  // namespace
 
 hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
-  // by the chunks of a row; the last takes rows of any length
+  // The smallest shape that holds the row; the last takes rows of any length. In bf16, T = 8192, by
+  // the shape that is taken and by the next one, us: V = 4095 59 and 64, 8191 87 and 102, 32767 236 and
+  // 263, 65535 452 and 556; V = 155647 at T = 4096 602 and 602.
+  //
+  // How many workgroups: one that takes row after row has the next row's loads in flight while it
+  // stores, and pays its start once; workgroups that start as others end keep the compute units evenly
+  // loaded. One workgroup per place / three per place / one per row, us: V = 4000 60 / 66 / 67 and 12000
+  // 122 / 123 / 140, V = 28000 208 / 198 / 204 and 40000 277 / 274 / 284, V = 50257 378 / 366 / 367 and
+  // 65535 476 / 461 / 452 (bf16, T = 8192), V = 106495 at T = 4096 412 / - / 451.
   static const Shape shapes[] = {
-      shape<64, 4, 0, 0>(),    shape<128, 4, 0, 0>(),   shape<128, 8, 0, 0>(),   shape<256, 8, 0, 0>(),
-      shape<256, 16, 0, 0>(),  shape<256, 24, 0, 0>(),  shape<512, 16, 0, 0>(),  shape<1024, 13, 0, 8>(),
-      shape<1024, 19, 0, 8>(), shape<1024, 16, 7, 0>()};
+      shape<64, 4, 0, 0>(1),    shape<128, 4, 0, 0>(1),  shape<128, 8, 0, 0>(1),  shape<256, 8, 0, 0>(1),
+      shape<256, 16, 0, 0>(3),  shape<256, 24, 0, 0>(3), shape<512, 16, 0, 0>(0), shape<1024, 13, 0, 8>(1),
+      shape<1024, 19, 0, 8>(1), shape<1024, 16, 7, 0>(1)};
   const int64_t chunks = (int64_t)a.V * (bf16 ? 2 : 4) / 16;
   const Shape* s = shapes;
   while (s + 1 < shapes + sizeof(shapes) / sizeof(shapes[0]) && (int64_t)s->nt * s->nc < chunks) ++s;
@@ -559,7 +573,7 @@ hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
   int64_t slots = 0;
   hipError_t e = resident_groups(fn, s->nt, &slots);
   if (e != hipSuccess) return e;
-  const int64_t grid = std::min<int64_t>(a.T, slots);
+  const int64_t grid = std::min<int64_t>(a.T, s->rounds ? s->rounds * slots : kMaxGrid);
   DistillArgs args = a;
   void* kargs[] = {&args};
   e = hipLaunchKernel(fn, dim3((unsigned)grid), dim3((unsigned)s->nt), kargs, 0, st);
