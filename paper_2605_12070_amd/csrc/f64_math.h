@@ -81,12 +81,9 @@ __device__ __forceinline__ double dpp_d(double v) {
   return f64_of(__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false),
                 __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, false));
 }
+// across the four rows of 16 lanes
 template <class F>
-__device__ __forceinline__ double wave_fold_f64(double v, F&& f) {
-  v = f(v, dpp_d<0xB1>(v));    // quad_perm [1,0,3,2]
-  v = f(v, dpp_d<0x4E>(v));    // quad_perm [2,3,0,1]
-  v = f(v, dpp_d<0x141>(v));   // row_half_mirror
-  v = f(v, dpp_d<0x140>(v));   // row_mirror
+__device__ __forceinline__ double wave_fold_rows(double v, F&& f) {
   uint64_t u = __builtin_bit_cast(uint64_t, v);
   auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
   auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
@@ -96,11 +93,31 @@ __device__ __forceinline__ double wave_fold_f64(double v, F&& f) {
   hi = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
   return f(f64_of(lo[0], hi[0]), f64_of(lo[1], hi[1]));
 }
+template <class F>
+__device__ __forceinline__ double wave_fold_f64(double v, F&& f) {
+  v = f(v, dpp_d<0xB1>(v));    // quad_perm [1,0,3,2]
+  v = f(v, dpp_d<0x4E>(v));    // quad_perm [2,3,0,1]
+  v = f(v, dpp_d<0x141>(v));   // row_half_mirror
+  v = f(v, dpp_d<0x140>(v));   // row_mirror
+  return wave_fold_rows(v, f);
+}
 __device__ __forceinline__ double wave_sum_f64(double v) {
   return wave_fold_f64(v, [](double a, double b) { return a + b; });
 }
 __device__ __forceinline__ double wave_max_f64(double v) {
   return wave_fold_f64(v, [](double a, double b) { return fmax(a, b); });
+}
+// Four wave-wide sums at less than half of four wave_sum_f64: in two steps each lane of a quad takes
+// over one of them. Lane i returns v[i & 3]'s.
+__device__ __forceinline__ double wave_sum4_f64(const double (&v)[4]) {
+  const int lane = (int)(threadIdx.x & 63);
+  const bool odd = lane & 1, upper = lane & 2;
+  const double a = (odd ? v[1] : v[0]) + dpp_d<0xB1>(odd ? v[0] : v[1]);       // from lane ^ 1
+  const double b = (odd ? v[3] : v[2]) + dpp_d<0xB1>(odd ? v[2] : v[3]);
+  double s = (upper ? b : a) + dpp_d<0x4E>(upper ? a : b);                     // from lane ^ 2
+  s += dpp_d<0x124>(s);        // row_ror:4
+  s += dpp_d<0x128>(s);        // row_ror:8
+  return wave_fold_rows(s, [](double x, double y) { return x + y; });
 }
 // A value that every lane of the wave holds, in scalar registers.
 __device__ __forceinline__ double wave_uniform(double v) {

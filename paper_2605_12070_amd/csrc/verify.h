@@ -36,7 +36,7 @@ struct VerifyDraw {
   int32_t reserved;
 };
 
-// Sums over a cell of a row drawn from.
+// Sums over a cell of a row drawn from (written as four doubles in this order).
 struct VerifyCell {
   double r;              // weights, with p and q as scaled
   double slope;          // q over the entries with a positive weight: d r / d (scale of q) = -slope

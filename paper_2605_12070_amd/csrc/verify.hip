@@ -31,7 +31,10 @@ constexpr int kStatsNT = 256;
 constexpr int kCellNT = 256;
 constexpr int kPickNT = 512;
 constexpr int kMaxParts = 16;
-constexpr int64_t kStatsRows = 512;   // rows of a launch of the statistics
+// Rows of a launch of the statistics. Larger launches read more rows behind a stop, smaller ones look
+// for the stops more often: 512, 1024 and 2048 take 204, 193 and 205 us at B = 256, D = 4, V = 151936 in
+// bf16 with 1.9 drafts of 4 accepted, 189, 187 and 208 us with 1.2 accepted.
+constexpr int64_t kStatsRows = 1024;
 
 template <typename Tin>
 __device__ __forceinline__ float entry_value(const Tin* p, int64_t i) {
@@ -72,6 +75,11 @@ __device__ __forceinline__ const Tin* draft_row(const VerifyArgs& a, int64_t b, 
   return (const Tin*)a.draft + b * a.draft_seq + i * a.draft_row;
 }
 
+// a / b: a 64-bit division is some 150 scalar instructions in a row, at the start of every workgroup
+__device__ __forceinline__ uint64_t divide(uint64_t a, uint32_t b) {
+  return a >> 32 ? a / b : (uint32_t)a / b;
+}
+
 // ------------------------------------------------------------------ where a sequence stops
 // A row's sum of exponentials as the statistics have it: log2 of it, and a bound on its error. Far
 // rows (logits past 2^20 log2 units, infinite ones and rows of nothing else than -inf or the type's
@@ -100,9 +108,9 @@ __device__ __forceinline__ void window_norms(const VerifyArgs& a, int64_t b, int
   const int lanes = a.parts > 8 ? 16 : a.parts > 4 ? 8 : a.parts > 2 ? 4 : a.parts;
   const int part = (int)threadIdx.x % lanes;
   const int rows = min(kWindow, n - from) + 1;       // of the target; the draft has none behind the last
-  for (int row = (int)threadIdx.x / lanes; row < 2 * (kWindow + 1); row += NT / lanes) {
+  for (int row = (int)threadIdx.x / lanes; row < 2 * rows; row += NT / lanes) {
     const int kind = row & 1, i = row >> 1;
-    const bool in = i < rows && (kind == 0 || (a.draft && from + i < n));
+    const bool in = kind == 0 || (a.draft && from + i < n);
     VerifyPart v = {-INFINITY, 0.0, -INFINITY};
     if (in && part < a.parts) v = a.stats[(((int64_t)(from + i) * a.B + b) * 2 + kind) * a.parts + part];
     double N = v.n, m = v.m;
@@ -132,18 +140,27 @@ __device__ __forceinline__ void window_norms(const VerifyArgs& a, int64_t b, int
 template <typename Tin, int NT>
 __device__ __forceinline__ Stop first_stop(const VerifyArgs& a, int b, int from, int n, bool write, StopState& st) {
   for (;; from += kWindow) {
+    // a draft per lane; what its decision reads is in flight together with the statistics
+    const int lane = threadIdx.x;
+    const int i = from + lane;
+    const bool in = lane < kWindow && i < n;
+    int64_t x = -1;
+    float u = 0.0f, zp = 0.0f, zq = 0.0f;
+    if (in) {
+      x = a.ids[(int64_t)b * a.D + i];
+      u = a.u[(int64_t)b * a.D + i];
+      if (x >= 0 && x < a.V) {
+        zp = entry_value(target_row<Tin>(a, b, i), x);
+        if (a.draft) zq = entry_value(draft_row<Tin>(a, b, i), x);
+      }
+    }
     __syncthreads();                                 // st is read
     window_norms<NT>(a, b, from, n, st);
     __syncthreads();
     if (threadIdx.x < 64) {
-      const int lane = threadIdx.x;
-      const int i = from + lane;
-      const bool in = lane < kWindow && i < n;
       int status = kAccept;
       float out = 0.0f;
-      int64_t x = -1;
       if (in) {
-        x = a.ids[(int64_t)b * a.D + i];
         const RowNorm p = st.norm[0][lane];
         RowNorm q{};
         if (a.draft) q = st.norm[1][lane];
@@ -152,11 +169,9 @@ __device__ __forceinline__ Stop first_stop(const VerifyArgs& a, int b, int from,
         } else if (p.far || q.far) {
           status = kUnclear;
         } else {
-          const float zp = entry_value(target_row<Tin>(a, b, i), x);
-          const float zq = a.draft ? entry_value(draft_row<Tin>(a, b, i), x) : 0.0f;
           const double lp = __builtin_fma((double)zp, a.t2e, -p.lse2);
           const double q_x = a.draft ? exp2_f64(__builtin_fma((double)zq, a.t2e, -q.lse2)) : 1.0;
-          const double uq = (double)a.u[(int64_t)b * a.D + i] * q_x, pp = exp2_f64(lp);
+          const double uq = (double)u * q_x, pp = exp2_f64(lp);
           const double mu = 1.0 + (p.err + q.err);
           status = uq * mu < pp ? kAccept : (uq < pp * mu ? kUnclear : kReject);
           if (pp == 0.0) status = kReject;
@@ -185,7 +200,7 @@ __device__ __forceinline__ Stop first_stop(const VerifyArgs& a, int b, int from,
 // One part of one row per workgroup, for the positions [i0, i1); positions outermost. Sequences that
 // clearly stop before i0 (whose statistics are complete: earlier launches) are skipped.
 template <typename Tin>
-__global__ __launch_bounds__(kStatsNT) void verify_stats(VerifyArgs a, int i0, int i1) {
+__global__ __launch_bounds__(kStatsNT, 4) void verify_stats(VerifyArgs a, int i0, int i1) {
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int NT = kStatsNT;
   constexpr int U = 8;
@@ -197,24 +212,26 @@ __global__ __launch_bounds__(kStatsNT) void verify_stats(VerifyArgs a, int i0, i
   const float L = (float)a.t2e;
   const int64_t items = (int64_t)(i1 - i0) * a.B * kinds * a.parts;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int part = (int)(item % a.parts);
-    const int64_t rest = item / a.parts;
-    const int kind = (int)(rest % kinds);
-    const int b = (int)((rest / kinds) % a.B);
-    const int i = i0 + (int)((rest / kinds) / a.B);
+    const uint64_t row = divide(item, a.parts);
+    const int part = (int)(item - row * a.parts);
+    const uint64_t pos_b = kinds == 2 ? row >> 1 : row;
+    const int kind = kinds == 2 ? (int)(row & 1) : 0;
+    const uint64_t pos = divide(pos_b, a.B);
+    const int b = (int)(pos_b - pos * a.B);
+    const int i = i0 + (int)pos;
     if (i + kind > drafts_of(a, b)) continue;        // uniform: not a row of this sequence
     const Tin* z = kind ? draft_row<Tin>(a, b, i) : target_row<Tin>(a, b, i);
     const RowSplit sp = split_row(z, a.V);
     const int c0 = (int)((int64_t)sp.nfull * part / a.parts);
     const int n = (int)((int64_t)sp.nfull * (part + 1) / a.parts) - c0;
     const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + sp.lead + (int64_t)c0 * E, n * 16);
-    uint32_t r[U][4];
-#pragma unroll
-    for (int u = 0; u < U; ++u) load16<kAuxLast>(r[u], rz, tid * 16, u * NT * 16);
     if (i0 > 0) {
       const int s = first_stop<Tin, NT>(a, b, 0, i0, false, st).status;
       if (s == kReject || s == kBadRow) continue;
     }
+    uint32_t r[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load16<kAuxLast>(r[u], rz, tid * 16, u * NT * 16);
     float N = kNoShift, m = -INFINITY;               // 2^N s so far; the largest logit
     double s = 0.0;
     auto add = [&](const auto& x) {
@@ -341,6 +358,19 @@ __device__ __forceinline__ void span_logits(const Tin* row, const CellSpan& s, b
   }
 }
 
+// 16 bytes of a row at any alignment, in a load of their own size
+typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
+template <typename Tin>
+__device__ __forceinline__ Words all_lowest() {
+  const uint32_t w = sizeof(Tin) == 2 ? 0xFF80FF80u : 0xFF800000u;   // -inf
+  return Words{w, w, w, w};
+}
+template <typename Tin>
+__device__ __forceinline__ void set_first(Words& w, Tin v) {
+  if constexpr (sizeof(Tin) == 2) w[0] = 0xFF800000u | v;
+  else w[0] = __float_as_uint(v);
+}
+
 // A row drawn from, and the workgroup's handle on it.
 template <typename Tin>
 struct DrawRows {
@@ -362,7 +392,7 @@ __device__ __forceinline__ DrawRows<Tin> draw_rows(const VerifyArgs& a, const Ve
 
 // ------------------------------------------------------------------ cells
 template <typename Tin>
-__global__ __launch_bounds__(kCellNT) void verify_cells(VerifyArgs a) {
+__global__ __launch_bounds__(kCellNT, 4) void verify_cells(VerifyArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int NW = kCellNT / 64;
   __shared__ double table[kExpTable];
@@ -373,8 +403,8 @@ __global__ __launch_bounds__(kCellNT) void verify_cells(VerifyArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   exp2_table_fill(table);
   for (int64_t item = blockIdx.x; item < (int64_t)a.B * a.draw_parts; item += gridDim.x) {
-    const int b = (int)(item / a.draw_parts);
-    const int part = (int)(item % a.draw_parts);
+    const int b = (int)divide(item, a.draw_parts);
+    const int part = (int)(item - (int64_t)b * a.draw_parts);
     const int n = drafts_of(a, b);
     // where the sequence stops; every workgroup of a sequence comes to the same answer
     VerifyDraw d{};
@@ -412,7 +442,7 @@ __global__ __launch_bounds__(kCellNT) void verify_cells(VerifyArgs a) {
       const RowNorm p = st.norm[0][d.pos - st.from];
       RowNorm q{};
       if (d.mode == kDrawResidual) q = st.norm[1][d.pos - st.from];
-      d.far = p.far || q.far;
+      d.far = __builtin_amdgcn_readfirstlane(p.far || q.far);
       if (p.bad || q.bad) d.mode = kDrawBad;
       if (d.far && d.mode != kDrawBad) {             // uniform
         d.p = exact_norm<Tin, kCellNT>(a, target_row<Tin>(a, b, d.pos), red);
@@ -430,24 +460,33 @@ __global__ __launch_bounds__(kCellNT) void verify_cells(VerifyArgs a) {
     const DrawRows<Tin> rows = draw_rows<Tin>(a, d, b);
     const int w0 = (int)((int64_t)a.cells * part / a.draw_parts);
     const int w1 = (int)((int64_t)a.cells * (part + 1) / a.draw_parts);
-    // the next cell's logits are read ahead
-    float zp[E], zq[E];
+    // The next cell's logits are read ahead, as they are; q's in p's chunks, whatever their alignment.
+    const Words low = all_lowest<Tin>();
+    Words wp, wq;
     auto fetch = [&](int cell) {
       const CellSpan s = cell < w1 ? cell_span<Tin>(rows.split, a.V, a.cells, cell, lane) : CellSpan{0, 0};
-      span_logits(rows.p, s, true, zp);
-      if (d.mode == kDrawResidual) span_logits(rows.q, s, rows.q_chunks, zq);
+      if (cell > 0 && cell < a.cells - 1) {          // uniform
+        // lanes past the chunks read the last one
+        const int e = rows.split.lead + (min((cell - 1) * 64 + lane, rows.split.nfull - 1)) * E;
+        wp = *(const u32x4*)(rows.p + e);
+        if (d.mode == kDrawResidual) wq = *(const Words*)(rows.q + e);
+      } else {
+        wp = wq = low;
+        if (s.count) {
+          set_first<Tin>(wp, rows.p[s.first]);
+          if (d.mode == kDrawResidual) set_first<Tin>(wq, rows.q[s.first]);
+        }
+      }
       return s;
     };
-    CellSpan s = fetch(w0 + wave);
+    CellSpan s = {0, 0};
+    if (w0 + wave < w1) s = fetch(w0 + wave);
     for (int cell = w0 + wave; cell < w1; cell += NW) {
       const CellSpan now = s;
       float cp[E], cq[E];
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        cp[j] = zp[j];
-        cq[j] = zq[j];
-      }
-      s = fetch(cell + NW);
+      unpack<Tin>(now.count ? wp : low, cp);
+      unpack<Tin>(now.count ? wq : low, cq);
+      if (cell + NW < w1) s = fetch(cell + NW);
       VerifyCell c = {0.0, 0.0, 0.0, 0.0};
       double w[E];
       probs(a, d, d.sp, d.p, cp, table, w);
@@ -463,15 +502,12 @@ __global__ __launch_bounds__(kCellNT) void verify_cells(VerifyArgs a) {
           c.r += r > 0.0 ? r : 0.0;
           c.slope += r > 0.0 ? v[j] : 0.0;
         }
-        c.q = wave_sum_f64(c.q);
-        c.slope = wave_sum_f64(c.slope);
       } else {
 #pragma unroll
         for (int j = 0; j < E; ++j) c.r += now.first + j == rows.x ? 0.0 : w[j];
       }
-      c.r = wave_sum_f64(c.r > kFlush ? c.r : 0.0);
-      c.p = wave_sum_f64(c.p > kFlush ? c.p : 0.0);
-      if (lane == 0) a.cell[(int64_t)b * a.cells + cell] = c;
+      const double sum = wave_sum4_f64({c.r > kFlush ? c.r : 0.0, c.slope, c.p > kFlush ? c.p : 0.0, c.q});
+      if (lane < 4) ((double*)(a.cell + (int64_t)b * a.cells + cell))[lane] = sum;
     }
   }
 }
@@ -491,6 +527,16 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
   const int wave = tid >> 6;
   exp2_table_fill(table);
   for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
+    // this thread's cells (consecutive), the first of them in registers, in flight together with the rest
+    // (all of them up to V = 2^20 bf16, 2^19 fp32)
+    constexpr int R = 4;
+    const VerifyCell* cells = a.cell + b * a.cells;
+    const int run = (a.cells + NT - 1) / NT;
+    const int r0 = min(tid * run, a.cells), r1 = min(r0 + run, a.cells);
+    VerifyCell own_cells[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) own_cells[k] = r0 + k < r1 ? cells[r0 + k] : VerifyCell{0.0, 0.0, 0.0, 0.0};
+    const double u_new = a.u_new[b];
     const VerifyDraw d = a.draw[b];
     int64_t* tokens = a.tokens + b * (a.D + 1);
     float* logp = a.logp + b * (a.D + 1);
@@ -506,14 +552,6 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
       }
       continue;
     }
-    const VerifyCell* cells = a.cell + b * a.cells;
-    const int run = (a.cells + NT - 1) / NT;         // cells per thread, consecutive
-    const int r0 = min(tid * run, a.cells), r1 = min(r0 + run, a.cells);
-    // the first of them in registers, loaded together (all of them up to V = 2^20 bf16, 2^19 fp32)
-    constexpr int R = 4;
-    VerifyCell own_cells[R];
-#pragma unroll
-    for (int k = 0; k < R; ++k) own_cells[k] = r0 + k < r1 ? cells[r0 + k] : VerifyCell{0.0, 0.0, 0.0, 0.0};
     // f(cell, its sums) over this thread's cells, until it returns true
     auto each = [&](auto&& f) {
       bool done = false;
@@ -580,7 +618,7 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
       residual = false;
       __syncthreads();
     }
-    const double goal = (double)a.u_new[b] * total;
+    const double goal = u_new * total;
     int hit_cell = a.cells;
     double hit_before = before;
     {
@@ -632,24 +670,36 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
       // no cell passed the goal (rounding, or u = 1): the last positive weight
       double c = (found_s < a.cells ? before_s : -INFINITY) + (incl - mine);
       int hit = -1, last = -1;
+      float z_hit = 0.0f, z_last = 0.0f;
 #pragma unroll
       for (int j = 0; j < E; ++j) {
         c += w[j];
         if (w[j] > 0.0) {
           last = s.first + j;
-          if (hit < 0 && c > goal) hit = last;
+          z_last = z[j];
+          if (hit < 0 && c > goal) {
+            hit = last;
+            z_hit = z[j];
+          }
         }
       }
       const uint64_t hits = __ballot(hit >= 0);
       const uint64_t lasts = __ballot(last >= 0);
       int v = -1;
-      if (hits) v = __shfl(hit, __builtin_ctzll(hits), 64);
-      else if (lasts) v = __shfl(last, 63 - __builtin_clzll(lasts), 64);
+      float zv = 0.0f;
+      if (hits) {
+        const int from = __builtin_ctzll(hits);
+        v = __shfl(hit, from, 64);
+        zv = __shfl(z_hit, from, 64);
+      } else if (lasts) {
+        const int from = 63 - __builtin_clzll(lasts);
+        v = __shfl(last, from, 64);
+        zv = __shfl(z_last, from, 64);
+      }
       if (lane == 0) {
         tokens[d.pos] = v;
         float out = __builtin_nanf("");
         if (v >= 0) {
-          const float zv = entry_value(rows.p, v);
           const double l = d.far ? log2_prob(a, d.p, zv)
                                  : __builtin_fma((double)zv, a.t2e, d.sp / kExpTable) - log2_f64(tp);
           out = (float)(l * kLn2F64);
@@ -668,9 +718,13 @@ int64_t verify_layout(VerifyArgs& a, int es, bool with_draft, void* workspace) {
   const int64_t chunks = a.V / E;
   const int64_t per = (int64_t)a.B * (with_draft ? 2 : 1);
   const int64_t rows = std::max<int64_t>(1, std::min<int64_t>(per * (a.D + 1), std::max<int64_t>(per, kStatsRows)));
-  // a part of two chunks per thread or more, while a launch's rows do not fill the device
-  a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxParts, 2048 / rows, chunks / (2 * kStatsNT)}));
+  // A part of two chunks per thread or more, while a launch's rows do not fill the device: 2048, 4096
+  // and 6144 workgroups take 107, 96 and 99 us at B = 128, D = 8, V = 100000 in bf16, 45, 45 and 49 us at
+  // B = 32, D = 5, V = 151936.
+  a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxParts, 4096 / rows, chunks / (2 * kStatsNT)}));
   a.cells = (int)((chunks + 63) / 64 + 2);
+  // Every workgroup of the weights first finds where its sequence stops. 512, 1024 and 2048 of them: 211,
+  // 198 and 201 us at B = 256, D = 4, V = 151936 in bf16, 49, 48 and 52 us at B = 64, V = 50257 in fp32.
   a.draw_parts = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / std::max(a.B, 1), a.cells / 8));
   int64_t o = 0;
   auto take = [&](int64_t bytes) {
