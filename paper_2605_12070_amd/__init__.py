@@ -751,9 +751,9 @@ def top_logits(logits: torch.Tensor, k: int, *, temperature: float = 1.0) -> Top
     ptr, T, V, ld = _matrix(_plain(logits, "logits"), "logits")
     dev = logits.device
     code = _dtype_code(logits)
-    n = _lib.lib().top_logits_workspace_bytes(code, T, V, int(k))
-    k = int(k)
-    rows = max(k, 0) if n >= 0 else 0          # sizes out of range: the call says which
+    k = max(0, min(int(k), _lib.MAX_TOP + 1))  # out of range stays out of range in 32 bits
+    n = _lib.lib().top_logits_workspace_bytes(code, T, V, k)
+    rows = k if n >= 0 else 0                  # sizes out of range: the call says which
     values = torch.empty(T, rows, dtype=torch.float32, device=dev)
     ids = torch.empty(T, rows, dtype=torch.int32, device=dev)
     lse = torch.empty(T, dtype=torch.float32, device=dev)

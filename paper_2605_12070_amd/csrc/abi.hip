@@ -1135,7 +1135,7 @@ dppo_status distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t T, i
   }
   hipStream_t st = (hipStream_t)stream;
   // a batch short enough for every workgroup to read its mask needs no counting kernel
-  const bool count_mode = T <= dppo::kCountModeMaxT;
+  const bool count_mode = T <= dppo::kDistillCountT;
   hipError_t e = hipSuccess;
   if (!count_mode && scale_mode == DPPO_SCALE_TOKEN_MEAN) {
     dppo::launch_prep_stats(loss_mask, T, stats_out, st);
