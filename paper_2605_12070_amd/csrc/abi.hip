@@ -1075,7 +1075,7 @@ int64_t top_logits_workspace_bytes(int32_t dtype, int64_t T, int64_t V, int32_t 
   if ((dtype != DPPO_F32 && dtype != DPPO_BF16) || T < 0 || T > 0x7FFFFFFF || V < 1 ||
       V > (int64_t)1 << 28 || k < 1 || k > DPPO_MAX_TOP || k > V)
     return -1;
-  const int parts = dppo::top_parts(T, V, esize_of(dtype));
+  const int parts = dppo::top_parts(T, V, esize_of(dtype), k);
   return parts > 1 ? top_cand_bytes(T, k, parts) + T * parts * 8 : 0;
 }
 
@@ -1097,7 +1097,7 @@ dppo_status top_logits(const void* logits, int32_t dtype, int64_t T, int64_t V, 
   a.T = (int32_t)T;
   a.V = (int32_t)V;
   a.k = k;
-  a.parts = dppo::top_parts(T, V, esize_of(dtype));
+  a.parts = dppo::top_parts(T, V, esize_of(dtype), k);
   a.l2e = (float)(1.44269504088896340736 / temperature);
   a.values = values_out;
   a.ids = ids_out;

@@ -19,8 +19,8 @@ struct TopArgs {
   float* part;         // parts > 1: [T, parts, 2] (n, s) of the parts' sums of exponentials
 };
 
-// Workgroups per row for a batch of T rows of V entries of es bytes.
-int top_parts(int64_t T, int64_t V, int es);
+// Workgroups per row for the k largest of T rows of V entries of es bytes.
+int top_parts(int64_t T, int64_t V, int es, int k);
 hipError_t launch_top_logits(const TopArgs& a, bool bf16, hipStream_t st);
 
 }  // namespace dppo

@@ -413,7 +413,6 @@ __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
 // chunks, or k close to their number) over the entries themselves.
 // ---------------------------------------------------------------------------------------
 constexpr int kShortCap = 512;
-constexpr int kShortRows = 512;
 
 template <typename Tin, int M>
 __global__ __launch_bounds__(64) void top_short(TopArgs a) {
@@ -583,10 +582,14 @@ __global__ __launch_bounds__(kJoinNT) void top_join(TopArgs a) {
 
 }  // namespace
 
-int top_parts(int64_t T, int64_t V, int es) {
-  // a part of at least 4096 chunks, while the rows do not fill the device twice
-  const int64_t most = std::min<int64_t>(kTopParts, V * es / (16 * 4096));
-  const int64_t want = T > 0 ? 512 / T : 1;
+int top_parts(int64_t T, int64_t V, int es, int k) {
+  // Parts of at least 2048 chunks and 16 chunks per entry asked for (a part brings k candidates to the
+  // join), while the rows do not fill the device four times. us, bf16: at least 2048 and 4096 chunks 21
+  // and 24 at T = 8, V = 151936, k = 64, 38 and 32 at T = 1, V = 33000, k = 256; 1024, 512 and 2048
+  // workgroups 40, 49 and 51 at T = 200, V = 262144, 65, 67 and 88 at T = 1000, V = 151936.
+  const int64_t least = std::max(2048, 16 * k);
+  const int64_t most = std::min<int64_t>(kTopParts, V * es / (16 * least));
+  const int64_t want = T > 0 ? 1024 / T : 1;
   return (int)std::max<int64_t>(1, std::min(most, want));
 }
 
@@ -594,10 +597,10 @@ hipError_t launch_top_logits(const TopArgs& a, bool bf16, hipStream_t st) {
   constexpr int NT = 512;
   const int64_t items = (int64_t)a.T * a.parts;
   const int64_t chunks = (int64_t)a.V * (bf16 ? 2 : 4) / 16;
-  // A wave per row where there are many short ones (against a workgroup per row, us; bf16, T = 8192):
-  // V = 2048, k = 16, 64, 250 23, 26, 53 against 72, 77, 177; V = 8192 63, 76, 112 against 81, 88, 131;
-  // T = 4, V = 8000, k = 20 18 against 11.
-  if (chunks <= 64 * 16 && a.T >= kShortRows) {      // parts is 1: top_parts
+  // A wave per row where there are many short ones. Against a workgroup per row, us, bf16: 256 chunks
+  // (V = 2000, k = 200) 21 and 28 at T = 300, 24 and 68 at T = 2000; 1000 chunks (V = 8000) with k = 20 28
+  // and 24 at T = 2000, 68 and 76 at T = 8192, with k = 200 37 and 52, 97 and 180.
+  if (chunks <= 64 * 16 && a.T >= (chunks <= 64 * 4 ? 256 : 2048)) {   // top_parts gives 1
     const unsigned g = (unsigned)std::min<int64_t>(a.T, kLaunchThreads / 64);
     if (chunks <= 64 * 4) {
       if (bf16) top_short<uint16_t, 4><<<g, 64, 0, st>>>(a);

@@ -131,11 +131,11 @@ def test_wide_records_of_long_rows(dtype, T, V, k):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [521, 2057])
 @pytest.mark.parametrize("V,k", [(40, 40), (300, 256), (1030, 3), (2051, 64), (4100, 200)])
-def test_many_short_rows(dtype, V, k):
-    """A wave per row: the same row kinds among many rows."""
-    print(f"[case] top short {dtype} V={V} k={k}", flush=True)
-    T = 512 + 9
+def test_many_short_rows(dtype, V, k, T):
+    """A wave per row where there are enough of them: the same row kinds among many rows."""
+    print(f"[case] top short {dtype} T={T} V={V} k={k}", flush=True)
     z = rows(T, V, dtype, seed=V, ld=V + 3, offset=1)
     inf = float("inf")
     z[0].fill_(2.5)
