@@ -33,7 +33,6 @@ struct VerifyDraw {
   int32_t pos;           // accepted drafts: the position drawn at
   int32_t mode;          // a VerifyMode
   int32_t far;
-  int32_t reserved;
 };
 
 // Sums over a cell of a row drawn from (written as four doubles in this order).
