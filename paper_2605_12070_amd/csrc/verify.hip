@@ -470,7 +470,8 @@ __global__ __launch_bounds__(kCellNT, 4) void verify_cells(VerifyArgs a) {
     Words wp, wq;
     auto fetch = [&](int cell) {
       const CellSpan s = cell < w1 ? cell_span<Tin>(rows.split, a.V, a.cells, cell, lane) : CellSpan{0, 0};
-      if (cell > 0 && cell < a.cells - 1) {          // uniform
+      // uniform; a row of fewer entries than fill a chunk at its offset has none
+      if (cell > 0 && cell < a.cells - 1 && rows.split.nfull > 0) {
         // lanes past the chunks read the last one
         const int e = rows.split.lead + (min((cell - 1) * 64 + lane, rows.split.nfull - 1)) * E;
         wp = *(const u32x4*)(rows.p + e);

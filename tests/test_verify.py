@@ -68,6 +68,21 @@ def test_strides_and_offsets(dtype, offset, q_offset):
     check(z.transpose(0, 1).contiguous().transpose(0, 1), ids, u, un, q)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [1, 3, 4, 5, 7, 8, 9, 11, 15, 16, 17, 23])
+def test_rows_around_one_chunk_at_every_offset(dtype, V):
+    """Rows that hold no whole 16-byte chunk at their offset, the draft's rows at an allocation's start."""
+    print(f"[case] verify chunk {dtype} V={V}", flush=True)
+    B, D = 3, 2
+    z, ids, u, un, q = inputs(B, D, V, dtype, seed=V)
+    for offset in range(8):
+        buf = torch.full((B * (D + 1) * V + 8,), 30.0, device=DEV).to(dtype)
+        zz = buf[offset:offset + z.numel()].view(z.shape)
+        zz.copy_(z)
+        check(zz, ids, u, un, q.clone())
+        check(zz, ids, u, un)
+
+
 @pytest.mark.parametrize("drafts", ["logits", "tokens"])
 def test_ends_of_the_random_numbers(drafts):
     """u of 0 and just below 1 (and 1, which is outside the range), drafts equal to the policy, drafts
