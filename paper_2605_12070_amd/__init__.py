@@ -820,7 +820,9 @@ def distill_loss_fwd_bwd(logits, teacher_values, teacher_ids, teacher_lse=None, 
 
 class DistillLoss(torch.autograd.Function):
     """Autograd wrapper: forward runs distill_loss_fwd_bwd (loss and dlogits at once); backward
-    returns grad_output * dlogits in one pass. The teacher's record gets no gradient."""
+    returns grad_output * dlogits in one pass. The teacher's record gets no gradient. Capture a
+    backward into a graph with no eager graph of the same leaves alive (PyTorch's rule: it ends the
+    process otherwise)."""
 
     @staticmethod
     def forward(ctx, logits, teacher_values, teacher_ids, teacher_lse, loss_mask, token_scale, kwargs):
