@@ -572,8 +572,14 @@ hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
       shape<256, 16, 0, 0>(3),  shape<256, 24, 0, 0>(3), shape<512, 16, 0, 0>(0), shape<1024, 13, 0, 8>(1),
       shape<1024, 19, 0, 8>(1), shape<1024, 16, 7, 0>(1)};
   const int64_t chunks = (int64_t)a.V * (bf16 ? 2 : 4) / 16;
+  // Few rows leave most of the device idle and wait for one row's steps: more threads share its chunks.
+  // 512 threads against the smallest shape, us, bf16: V = 32000 20 and 25 at T = 64, 27 and 30 at T = 512,
+  // 46 and 40 at T = 1024; V = 10000 18 and 20 at T = 256, 34 and 25 at T = 1000.
+  const int least = a.T <= 512 ? 512 : 64;
   const Shape* s = shapes;
-  while (s + 1 < shapes + sizeof(shapes) / sizeof(shapes[0]) && (int64_t)s->nt * s->nc < chunks) ++s;
+  while (s + 1 < shapes + sizeof(shapes) / sizeof(shapes[0]) &&
+         ((int64_t)s->nt * s->nc < chunks || s->nt < least))
+    ++s;
   const void* fn = bf16 ? s->bf16 : s->f32;
   int64_t slots = 0;
   hipError_t e = resident_groups(fn, s->nt, &slots);

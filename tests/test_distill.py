@@ -243,3 +243,42 @@ def test_another_stream_and_the_same_bits_again():
     s.synchronize()
     for x, y in ((a.loss, b.loss), (a.kl, b.kl), (a.dlogits, b.dlogits), (a.stats, b.stats)):
         assert torch.equal(x, y)
+
+
+# rows enough for the shapes of fewer threads: their capacities, rows that start anywhere, more rows than
+# fit on the device at once
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("chunks,T,k", [(3, 600, 2), (250, 600, 20), (40, 20000, 5), (256, 9000, 64), (511, 700, 100), (900, 5000, 9),
+                                        (1024, 600, 256), (2047, 530, 30), (4095, 1600, 65), (4096, 520, 3), (6143, 530, 200),
+                                        (8191, 530, 12)])
+def test_many_rows(dtype, chunks, T, k):
+    V = chunks * (8 if dtype == BF else 4) - 1 + chunks % 3
+    print(f"[case] distill rows {dtype} T={T} V={V} k={k}", flush=True)
+    few = 7
+    z7 = rows(few, V, dtype, seed=V)
+    values, ids, lse = record(z7, k, V)
+    z = z7[torch.arange(T, device=DEV) % few]                  # rows of an odd length start anywhere
+    many = [t[torch.arange(T, device=DEV) % few] for t in (values, ids, lse)]
+    mask = (torch.arange(T, device=DEV) % 11 != 3).to(torch.uint8)
+    ref = oracle.distill_loss(values_of(z7), values.cpu().numpy(), ids.cpu().numpy(), lse.cpu().double().numpy(), scale_mode="const")
+    d = torch.full((T, V + 3), 5.0, dtype=dtype, device=DEV)
+    r = P.distill_loss_fwd_bwd(z, *many, mask, scale_mode="const", dlogits=d[:, 1:V + 1])
+    on = mask.bool()
+    kl = torch.from_numpy(ref["kl"]).to(DEV)
+    want = torch.from_numpy(ref["dlogits"]).to(DEV)
+    tol = U[dtype] * want.abs() + GRAD * torch.from_numpy(ref["slack"]).to(DEV) + 2.0 ** -126
+    assert bool((r.flags == mask).all()) and int(r.stats[0]) == int(on.sum())
+    assert bool((d[:, 0] == 5.0).all()) and bool((d[:, V + 1:] == 5.0).all())
+    for c in range(few):                                       # the rows of one content
+        t = torch.arange(c, T, few, device=DEV)
+        live, dead = t[on[t]], t[~on[t]]
+        assert float((r.kl[live].double() - kl[c]).abs().max()) <= KL * max(1.0, abs(float(kl[c])))
+        assert bool((r.kl[dead] == 0).all()) and bool((d[dead, 1:V + 1] == 0).all())
+        for part in live.split(64):
+            assert bool(((d[part, 1:V + 1].double() - want[c]).abs() <= tol[c]).all()), (c, part)
+    total = sum(float(kl[c]) * int(on[torch.arange(c, T, few, device=DEV)].sum()) for c in range(few))
+    assert abs(float(r.loss) - total) <= 2 * KL * T * max(1.0, float(kl.abs().max()))
+    in_place = P.distill_loss_fwd_bwd(z, *many, mask, scale_mode="const", dlogits=z)
+    got = in_place.dlogits[on][:50].double()
+    c = (torch.arange(T, device=DEV) % few)[on][:50]
+    assert bool(((got - want[c]).abs() <= tol[c]).all())
