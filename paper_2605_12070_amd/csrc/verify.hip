@@ -129,11 +129,12 @@ __device__ __forceinline__ void window_norms(const VerifyArgs& a, int64_t b, int
     RowNorm r;
     r.far = !(fabs(m) * a.t2e < 1048576.0);
     r.bad = !r.far && !(s > 0.0 && s < INFINITY);
-    r.lse2 = r.far || r.bad ? 0.0 : N + log2_f64(s);
-    // Terms: the exponential (2^-22) and a chunk's additions (2^-22); its argument's rounding, 2^-24 of
-    // log2 units below the maximum, which weighs at most log2(V) <= 28 over the row; the 32-bit log2(e)
-    // / temperature, 2^-25 of the logits that matter. In all below 2.7e-6 + |m t2e| 2^-24 of the sum.
-    r.err = 8e-6 + fabs(r.lse2) * 2.4e-7;
+    // the sums took log2(e) / temperature in 32 bits: the logits that matter lie next to m
+    r.lse2 = r.far || r.bad ? 0.0 : N + log2_f64(s) - m * ((double)(float)a.t2e - a.t2e);
+    // Terms: the exponential (2^-22) and a chunk's additions (2^-22); its argument's rounding and that of
+    // log2(e) / temperature, 2^-24 each of the log2 units below the maximum, which weigh at most log2(V) <=
+    // 28 over the row. In all below 2.9e-6 of the sum.
+    r.err = 8e-6;
     st.norm[kind][i] = r;
   }
 }
@@ -334,6 +335,45 @@ __device__ __forceinline__ void probs(const VerifyArgs& a, const VerifyDraw& d, 
   }
 }
 
+// exact_norm of a row whose log2 sum is about lse2 and not large, from weights as above: a fifth of its
+// time (which some percent of large batches wait for, each decision with a chance of some 1e-5).
+template <typename Tin, int NT>
+__device__ VerifyNorm near_norm(const VerifyArgs& a, const Tin* z, double lse2, const double* table, double* red) {
+  constexpr int NW = NT / 64;
+  constexpr int E = 16 / (int)sizeof(Tin);
+  constexpr int U = 2;
+  const int tid = threadIdx.x;
+  const double shift = -__builtin_rint(lse2 * kExpTable), K = a.t2e * kExpTable, sm = shift + kRoundMagic;
+  const float low = lowest_logit(a, shift);
+  const RowSplit sp = split_row(z, a.V);
+  const __amdgpu_buffer_rsrc_t rz = row_rsrc(z + sp.lead, sp.nfull * 16);
+  double s = 0.0;
+  auto add = [&](float x) { s += exp2_tab((double)__builtin_elementwise_maximum(x, low), K, sm, table); };
+  if (tid < sp.nedge) add(entry_value(z, sp.template entry<E>(tid)));
+#pragma unroll 1
+  for (int c = tid; c < sp.nfull; c += U * NT) {
+    uint32_t r[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load16<kAuxLast>(r[u], rz, c * 16, u * NT * 16);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (c + u * NT >= sp.nfull) break;
+      float x[E];
+      unpack<Tin>(r[u], x);
+#pragma unroll
+      for (int j = 0; j < E; ++j) add(x[j]);
+    }
+  }
+  s = wave_sum_f64(s);
+  __syncthreads();
+  if ((tid & 63) == 0) red[tid >> 6] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int w = 0; w < NW; ++w) s += red[w];
+  __syncthreads();
+  return {0.0, s > 0.0 && s < INFINITY ? log2_f64(s) - shift / kExpTable : (double)__builtin_nanf("")};
+}
+
 // Cell 0 holds the entries before the target row's whole chunks, cell c the 64 chunks from 64 (c - 1)
 // on, the last cell the entries behind them. A lane's entries of a cell: `count` of them (a chunk or a
 // single one) from `first` on.
@@ -423,12 +463,17 @@ __global__ __launch_bounds__(kCellNT, 4) void verify_cells(VerifyArgs a) {
       // within the statistics' error, or beyond their range: from exact sums over the two rows
       const int64_t x = a.ids[(int64_t)b * a.D + s.pos];
       const Tin* p = target_row<Tin>(a, b, s.pos);
-      d.p = exact_norm<Tin, kCellNT>(a, p, red);
+      // (log2s alone holds 2^-40 of a probability where it is below 4096)
+      auto norm_of = [&](const Tin* z, const RowNorm& n) {
+        return !n.far && fabs(n.lse2) < 4096.0 ? near_norm<Tin, kCellNT>(a, z, n.lse2, table, red)
+                                               : exact_norm<Tin, kCellNT>(a, z, red);
+      };
+      d.p = norm_of(p, st.norm[0][s.pos - st.from]);
       d.q = {0.0, 0.0};
       double q = 1.0;
       if (a.draft) {
         const Tin* qr = draft_row<Tin>(a, b, s.pos);
-        d.q = exact_norm<Tin, kCellNT>(a, qr, red);
+        d.q = norm_of(qr, st.norm[1][s.pos - st.from]);
         q = exp2_f64(log2_prob(a, d.q, entry_value(qr, x)));
       }
       const double lp = log2_prob(a, d.p, entry_value(p, x));

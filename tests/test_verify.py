@@ -84,6 +84,31 @@ def test_rows_around_one_chunk_at_every_offset(dtype, V):
 
 
 @pytest.mark.parametrize("drafts", ["logits", "tokens"])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,D,V,offset,shift", [(6, 3, 40, 0, 0.0), (5, 4, 1003, 1, 20.0), (4, 20, 5001, 3, -900.0),
+                                                (3, 3, 50257, 0, 5000.0), (2, 3, 151936, 2, 0.0)])
+def test_decisions_next_to_their_border(dtype, drafts, B, D, V, offset, shift):
+    """Random numbers within a float's step of p / q: the 32-bit statistics cannot tell."""
+    print(f"[case] verify border {dtype} {drafts} B={B} D={D} V={V}", flush=True)
+    z, ids, u, un, q = inputs(B, D, V, dtype, seed=V + B, drafts=drafts, sigma=2.0)
+    z = (z.float() + shift).to(dtype)
+    buf = torch.zeros(z.numel() + 8, dtype=dtype, device=DEV)
+    zz = buf[offset:offset + z.numel()].view(z.shape)
+    zz.copy_(z)
+    f = lambda t, i: np.take_along_axis(np.apply_along_axis(oracle.dppo_oracle.log_softmax_row, 2, values_of(  # noqa: E731
+        t.reshape(-1, V)).reshape(t.shape)[:, :D]), i, 2)[:, :, 0]
+    i = ids.cpu().numpy()[:, :, None]
+    ratio = np.exp(f(z, i) - (f(q, i) if q is not None else 0.0))
+    x = np.minimum(ratio, 1.0).astype(np.float32)
+    steps = np.random.default_rng(V).integers(-1, 2, x.shape)
+    x = np.where(steps > 0, np.nextafter(x, np.float32(2)), np.where(steps < 0, np.nextafter(x, np.float32(0)), x))
+    margin = np.abs(x.astype(np.float64) / ratio - 1.0)
+    # The inputs: decidable by sums of exponentials good to 4.5e-12 over two rows (9e-12), not in 32 bits.
+    assert margin.min() > 2e-11 and (margin < 2e-7).any()
+    check(zz, ids, torch.from_numpy(x).to(DEV), un, q)
+
+
+@pytest.mark.parametrize("drafts", ["logits", "tokens"])
 def test_ends_of_the_random_numbers(drafts):
     """u of 0 and just below 1 (and 1, which is outside the range), drafts equal to the policy, drafts
     the policy rules out."""
