@@ -6,9 +6,9 @@
 // workgroup streams a row in tiles of U 16-byte chunks per thread; after the first tile, and each
 // time the part read has doubled, it takes that bound from the maxima so far, and chunks with an entry
 // that reaches the bound of their time are kept in LDS (about k (1 + ln tiles) of them in random
-// order). At the end the kept chunks' entries that reach the last bound are ranked by counting. What the fast path cannot hold (long runs of
-// equal values, a row with NaN or infinities, fewer than k finite entries) is selected exactly by
-// radix passes over the row.
+// order). At the end the kept chunks' entries that reach the last bound are ranked by counting. What the
+// fast path cannot hold (long runs of equal values, a row with NaN or infinities, fewer than k finite
+// entries) is selected exactly by radix passes over the row.
 //
 // Long rows in a batch that fills the device are bound by HBM: T = 8192, V = 151936 bf16, k = 64 takes 436
 // us, 5.7 TB/s of logits; T = 2048, V = 50257 fp32, k = 128 takes 90 us, 4.6 TB/s, a quarter of it the

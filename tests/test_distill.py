@@ -248,9 +248,10 @@ def test_another_stream_and_the_same_bits_again():
 # rows enough for the shapes of fewer threads: their capacities, rows that start anywhere, more rows than
 # fit on the device at once
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("chunks,T,k", [(3, 600, 2), (250, 600, 20), (40, 20000, 5), (256, 9000, 64), (511, 700, 100), (900, 5000, 9),
-                                        (1024, 600, 256), (2047, 530, 30), (4095, 1600, 65), (4096, 520, 3), (6143, 530, 200),
-                                        (8191, 530, 12)])
+@pytest.mark.parametrize("chunks,T,k", [
+    (3, 600, 2), (250, 600, 20), (40, 20000, 5), (256, 9000, 64), (511, 700, 100), (900, 5000, 9), (1024, 600, 256),
+    (2047, 530, 30), (4095, 1600, 65), (4096, 520, 3), (6143, 530, 200), (8191, 530, 12),
+])
 def test_many_rows(dtype, chunks, T, k):
     V = chunks * (8 if dtype == BF else 4) - 1 + chunks % 3
     print(f"[case] distill rows {dtype} T={T} V={V} k={k}", flush=True)
@@ -260,7 +261,8 @@ def test_many_rows(dtype, chunks, T, k):
     z = z7[torch.arange(T, device=DEV) % few]                  # rows of an odd length start anywhere
     many = [t[torch.arange(T, device=DEV) % few] for t in (values, ids, lse)]
     mask = (torch.arange(T, device=DEV) % 11 != 3).to(torch.uint8)
-    ref = oracle.distill_loss(values_of(z7), values.cpu().numpy(), ids.cpu().numpy(), lse.cpu().double().numpy(), scale_mode="const")
+    ref = oracle.distill_loss(values_of(z7), values.cpu().numpy(), ids.cpu().numpy(), lse.cpu().double().numpy(),
+                              scale_mode="const")
     d = torch.full((T, V + 3), 5.0, dtype=dtype, device=DEV)
     r = P.distill_loss_fwd_bwd(z, *many, mask, scale_mode="const", dlogits=d[:, 1:V + 1])
     on = mask.bool()
