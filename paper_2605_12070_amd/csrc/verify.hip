@@ -436,6 +436,7 @@ __device__ __forceinline__ DrawRows<Tin> draw_rows(const VerifyArgs& a, const Ve
 }
 
 // ------------------------------------------------------------------ cells
+// 128 registers: at 96 (five waves per SIMD) it spills, and 199 us become 214 (B = 256, D = 4, V = 151936).
 template <typename Tin>
 __global__ __launch_bounds__(kCellNT, 4) void verify_cells(VerifyArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
