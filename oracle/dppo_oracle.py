@@ -603,9 +603,7 @@ def distill_loss(z, values, ids, lse=None, mask=None, token_scale=None, tau=1.0,
             flags[t] |= FLAG_BAD_ID
             continue
         with np.errstate(all="ignore"):
-            x = z[t] / tau
-            norm = row_logsumexp(x[None])[0]
-            logq = x - norm
+            logq = log_softmax_row(z[t] / tau)
             q = np.exp(logq)
             entries = [j for j in range(ids.shape[1]) if ids[t, j] >= 0]
             tt = values[t, entries] / tau

@@ -1098,7 +1098,8 @@ dppo_status top_logits(const void* logits, int32_t dtype, int64_t T, int64_t V, 
   a.V = (int32_t)V;
   a.k = k;
   a.parts = dppo::top_parts(T, V, esize_of(dtype), k);
-  a.l2e = (float)(1.44269504088896340736 / temperature);
+  a.t2e = 1.44269504088896340736 / temperature;
+  a.l2e = (float)a.t2e;
   a.values = values_out;
   a.ids = ids_out;
   a.lse = lse_out;

@@ -57,6 +57,7 @@ struct RecordMath {    // one row at a time, between two barriers
   float z[kMaxK];      // the student's logits, then its probabilities q
   int any_again;
   float w, lse2;
+  int far;             // the row's sum in 32 bits says nothing (kFarLog2)
 };
 
 // The record's part of a row, by one wave: lane holds entries lane, lane + 64, ... N, S: the sum of
@@ -136,8 +137,86 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
     // what rounding lse2 to 32 bits leaves over goes into the factor
     const float l2 = (float)lse2;
     m.lse2 = l2;
+    // zm is the row's maximum; entries outside the record that lie far below it weigh nothing
+    m.far = !(S < INFINITY) || (fabs(zm) >= (double)kFarLog2 && zm != -INFINITY);
     m.w = (float)(s * f * exp2_f64((double)l2 - lse2));
     a.loss_tok[row] = (float)l;
+  }
+}
+
+template <typename Tin>
+__device__ __forceinline__ float entry_value(const Tin* p, int64_t i) {
+  if constexpr (sizeof(Tin) == 2) return bf16_to_f32(p[i]);
+  else return p[i];
+}
+
+// A far row (kFarLog2), from its logits in memory: their differences to the row's maximum take their place
+// (both give the same softmax), in 64 bits in the sum. A row holding NaN or +inf, or only -inf, keeps
+// its logits and comes out NaN. By the whole workgroup, once its other rows are done; thread tid has the entries
+// tid, tid + NT, ...; red holds a double per wave.
+constexpr uint8_t kFlagFar = 0x80;       // in flags_out until the row's turn comes
+template <typename Tin, int NT>
+__device__ __forceinline__ void far_row(const DistillArgs& a, int64_t row, float scale, Record<NT>& rec, RecordMath& m,
+                                     double* red) {
+  constexpr int NW = NT / 64;
+  const int tid = threadIdx.x;
+  const Tin* z = (const Tin*)a.logits + row * a.ld;
+  Tin* d = a.dlogits ? (Tin*)a.dlogits + row * a.ldd : nullptr;
+  const int V = a.V;
+  __syncthreads();                         // the last row's LDS is free
+  rec.head[tid] = -1;
+  if (tid == 0) m.any_again = 0;
+  __syncthreads();
+  for (int j = tid; j < a.k; j += NT) {
+    const int id = a.tokens[row * a.k + j];
+    rec.id[j] = id;
+    rec.again[j] = 0;
+    m.value[j] = id < 0 ? -INFINITY : a.values[row * a.k + j];
+    if (id >= 0) rec.next[j] = (int16_t)atomicExch(&rec.head[id % NT], j);
+  }
+  float base = -INFINITY;
+  for (int e = tid; e < V; e += NT) {
+    const float x = entry_value(z, e);
+    base = x != x ? INFINITY : fmaxf(base, x);
+  }
+  base = wave_max(base);
+  if ((tid & 63) == 0) red[tid >> 6] = base;
+  __syncthreads();
+  for (int w = 0; w < NW; ++w) base = fmaxf(base, (float)red[w]);
+  if (!(fabsf(base) < INFINITY)) base = 0.0f;
+  const int head = rec.head[tid];
+  for (int j = head; j >= 0; j = rec.next[j])
+    for (int j2 = rec.next[j]; j2 >= 0; j2 = rec.next[j2])
+      if (rec.id[j2] == rec.id[j]) {
+        rec.again[j > j2 ? j : j2] = 1;
+        m.any_again = 1;
+      }
+  auto place = [&](int e) {                // of an entry in the record, -1: none
+    int at = -1;
+    for (int j = head; j >= 0; j = rec.next[j])
+      if (rec.id[j] == e && !rec.again[j]) at = j;
+    return at;
+  };
+  double s = 0.0;
+  for (int e = tid; e < V; e += NT)
+    if (place(e) < 0) s += exp2_f64((double)(entry_value(z, e) - base) * (double)a.l2e);
+  s = wave_sum_f64(s);
+  for (int j = tid; j < a.k; j += NT) m.z[j] = rec.id[j] < 0 ? -INFINITY : entry_value(z, rec.id[j]) - base;
+  __syncthreads();                         // red is read
+  if ((tid & 63) == 0) red[tid >> 6] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int w = 0; w < NW; ++w) s += red[w];
+  if (tid < 64) record_math(a, row, scale * (a.tscale ? uload(a.tscale + row) : 1.0f), 0.0f, (float)s, rec, m);
+  if (tid == 0) a.flags[row] = (uint8_t)DPPO_FLAG_VALID;
+  __syncthreads();
+  if (!d) return;
+  const float w = m.w, l2 = m.lse2;
+  for (int e = tid; e < V; e += NT) {
+    const int j = place(e);
+    const float o = j >= 0 ? rec.grad[j] : w * exp2_hw(__builtin_fmaf(entry_value(z, e) - base, a.l2e, -l2));
+    if constexpr (sizeof(Tin) == 2) d[e] = to_bf16(o);
+    else d[e] = o;
   }
 }
 
@@ -146,8 +225,9 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
 // registers once this row's stores are out. Vector memory operations are waited for in the order they
 // were issued, so whatever a row waits for in its middle (the student's logits at the record's tokens,
 // its single entries) is issued before those loads, from ids that were loaded a row earlier.
+// The waves per SIMD are named since the compiler otherwise takes 149 registers where 127 do (NC = 16).
 template <typename Tin, int NT, int NC, int KS, int PF>
-__global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
+__global__ __launch_bounds__(NT, NC == 4 ? 5 : NC == 24 ? 3 : 4) void distill_rows(DistillArgs a) {
   static_assert(PF <= NC && (KS == 0 || PF == 0));
   constexpr int KE = (kMaxK + NT - 1) / NT;   // entries of a record per thread: tid, tid + NT, ...
   constexpr int E = 16 / (int)sizeof(Tin);
@@ -156,12 +236,15 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
   constexpr int kRecs = NT == 64 ? 1 : 2;     // one wave is never in two rows
   __shared__ Record<NT> recs[kRecs];
   __shared__ RecordMath rm;
+  __shared__ double far_red[NT / 64];
+  __shared__ int far_rows;
   __shared__ u32x4 keep[KS > 0 ? KS * NT : 1];
   __shared__ u32x4 ahead[PF > 0 ? PF * NT : 1];   // [chunk][thread]: a wave reads what it loaded
   const int tid = threadIdx.x;
   const int V = a.V;
   const float L = a.l2e;
   recs[0].head[tid] = recs[kRecs - 1].head[tid] = -1;
+  if (tid == 0) far_rows = 0;
   auto is_valid = [&](int64_t row) { return a.mask == nullptr || uload_u8(a.mask + row) != 0; };
   uint32_t r[NC][4];
   auto load_row = [&](int64_t row, bool rd) {
@@ -372,13 +455,16 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
       N = shift_of(N);
       block_merge_ns_int<NT>(N, S, red[parity]);
       if (tid < 64) record_math(a, row, scale * (a.tscale ? uload(a.tscale + row) : 1.0f), N, S, rec, rm);
-      if (tid == 0) a.flags[row] = (uint8_t)DPPO_FLAG_VALID;
+      if (tid == 0) {
+        a.flags[row] = rm.far ? kFlagFar : (uint8_t)DPPO_FLAG_VALID;
+        far_rows |= rm.far;
+      }
       __syncthreads();
     }
     load_ahead(next, next_valid);
     if (!good) {
       if (drow) zero_row<Tin, NT>(drow, V);
-    } else if (drow) {
+    } else if (drow && !rm.far) {          // uniform
       {
         const float w = rm.w, l2 = rm.lse2;
         const __amdgpu_buffer_rsrc_t rd = row_rsrc(drow + sp.lead, nfull * 16);
@@ -450,6 +536,11 @@ __global__ __launch_bounds__(NT) void distill_rows(DistillArgs a) {
     }
     load_row(next, next_valid);
     valid = next_valid;
+  }
+  __syncthreads();
+  if (far_rows) {                          // uniform
+    for (row = blockIdx.x; row < a.T; row += gridDim.x)
+      if (a.flags[row] == kFlagFar) far_row<Tin, NT>(a, row, scale, recs[0], rm, far_red);
   }
 }
 

@@ -109,6 +109,10 @@ __device__ __forceinline__ void add_logits(float& n, Sum& s, const float (&x)[E]
   s = s * (Sum)exp2_hw(n - N) + (Sum)c;
   n = N;
 }
+// From this many log2 units on a rounded product z L says too little of the exact one for the
+// exponentials next to it (half a step of it is 64 or more): rows whose maximum lies past it on either
+// side, and rows whose sum is not a positive number, are evaluated around their maximum in 64 bits.
+constexpr float kFarLog2 = 1073741824.0f;   // 2^30
 // The sum's shift, or -inf while nothing has been added.
 __device__ __forceinline__ float shift_of(float n) { return n == kNoShift ? -INFINITY : n; }
 

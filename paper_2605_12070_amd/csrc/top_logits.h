@@ -12,6 +12,7 @@ struct TopArgs {
   int32_t T, V, k;
   int32_t parts;       // workgroups per row
   float l2e;           // log2(e) / temperature
+  double t2e;          // the same in 64 bits, for far rows
   float* values;       // [T, k]
   int32_t* ids;        // [T, k]
   float* lse;          // [T]

@@ -20,6 +20,7 @@
 
 #include "dppo.h"
 #include "dppo_device.h"
+#include "f64_math.h"
 #include "row_split.h"
 
 namespace dppo {
@@ -185,6 +186,39 @@ __device__ __noinline__ void select_exact(const Tin* z, int e0, int e1, int kk, 
   }
 }
 
+// Whether a row's sum 2^N S in 32 bits is its sum of exponentials (uniform).
+__device__ __forceinline__ bool near_row(float N, float S) { return S > 0.0f && S < INFINITY && fabsf(N) < kFarLog2; }
+
+// The log-sum-exp of a far row, around its maximum in 64 bits; NaN for a row holding NaN or +inf, or only
+// -inf. By the whole workgroup; red holds a double per wave, and is free on return.
+template <typename Tin, int NT>
+__device__ __noinline__ float far_lse(const Tin* z, int V, double t2e, double* red) {
+  constexpr int NW = NT / 64;
+  const int wave = threadIdx.x >> 6;
+  float m = -INFINITY;
+  for (int e = threadIdx.x; e < V; e += NT) {
+    const float x = entry_value(z, e);
+    m = x != x ? INFINITY : fmaxf(m, x);
+  }
+  m = wave_max(m);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[wave] = m;
+  __syncthreads();
+  double M = red[0];
+  for (int w = 1; w < NW; ++w) M = fmax(M, red[w]);
+  __syncthreads();
+  if (fabs(M) == INFINITY) return __builtin_nanf("");
+  double s = 0.0;
+  for (int e = threadIdx.x; e < V; e += NT) s += exp2_f64(((double)entry_value(z, e) - M) * t2e);
+  s = wave_sum_f64(s);
+  if ((threadIdx.x & 63) == 0) red[wave] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int w = 0; w < NW; ++w) s += red[w];
+  __syncthreads();
+  return (float)(__builtin_fma(M, t2e, log2_f64(s)) * kLn2F64);
+}
+
 template <typename Tin, int NT>
 __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
@@ -193,7 +227,7 @@ __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
   __shared__ u32x4 chunk[kTopChunks];     // kept chunks; later the thinned-out entries
   __shared__ int chunk_at[kTopChunks];    // entry that a kept chunk starts at
   __shared__ uint64_t cand[kTopCap];
-  __shared__ uint32_t tkey[NT];
+  __shared__ alignas(16) uint32_t tkey[NT];
   __shared__ float red[2 * NW];
   __shared__ int wcount[NW];
   __shared__ int chunks, chunks_s, count, kcount;
@@ -400,13 +434,15 @@ __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
       if (rank < k) put(a, row, part, rank, c);
     }
     for (int i = kk + tid; i < k; i += NT) put(a, row, part, i, 0);   // a part shorter than k
-    if (tid == 0) {
-      if (a.parts > 1) {
+    if (a.parts > 1) {
+      if (tid == 0) {
         a.part[2 * item] = N;
         a.part[2 * item + 1] = S;
-      } else {
-        a.lse[row] = (N == -INFINITY) ? __builtin_nanf("") : (N + log2f(S)) * kLn2;
       }
+    } else {
+      float lse = (N + log2f(S)) * kLn2;
+      if (!near_row(N, S)) lse = far_lse<Tin, NT>(z, a.V, a.t2e, (double*)tkey);
+      if (tid == 0) a.lse[row] = lse;
     }
   }
 }
@@ -424,7 +460,7 @@ __global__ __launch_bounds__(64) void top_short(TopArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr uint32_t kKeyInf = 0xFF800000u;          // the key of +inf
   __shared__ uint64_t cand[kShortCap];
-  __shared__ int hist[256];
+  __shared__ alignas(16) int hist[256];
   __shared__ int count, wcount;
   const int lane = threadIdx.x;
   const uint64_t below = (1ull << lane) - 1ull;
@@ -527,7 +563,9 @@ __global__ __launch_bounds__(64) void top_short(TopArgs a) {
     sort_list(cand, n);
     __syncthreads();
     for (int i = lane; i < k; i += 64) put(a, row, 0, i, cand[i]);
-    if (lane == 0) a.lse[row] = (N == -INFINITY) ? __builtin_nanf("") : (N + log2f(S)) * kLn2;
+    float lse = (N + log2f(S)) * kLn2;
+    if (!near_row(N, S)) lse = far_lse<Tin, 64>(z, a.V, a.t2e, (double*)hist);
+    if (lane == 0) a.lse[row] = lse;
     __syncthreads();                       // cand is read
   }
 }
@@ -537,9 +575,11 @@ __global__ __launch_bounds__(64) void top_short(TopArgs a) {
 constexpr int kJoinNT = 512;
 constexpr int kTopParts = 16;
 
+template <typename Tin>
 __global__ __launch_bounds__(kJoinNT) void top_join(TopArgs a) {
   __shared__ uint64_t list[kTopParts * DPPO_MAX_TOP];
   __shared__ uint64_t kept[kTopParts * DPPO_MAX_TOP];
+  __shared__ double red[kJoinNT / 64];
   __shared__ int count;
   const int tid = threadIdx.x;
   const int k = a.k;
@@ -549,10 +589,9 @@ __global__ __launch_bounds__(kJoinNT) void top_join(TopArgs a) {
     __syncthreads();
     if (tid == 0) count = 0;
     for (int i = tid; i < m; i += kJoinNT) list[i] = a.cand[row * m + i];
-    float N = -INFINITY, S = 0.0f;
-    if (tid == 0)
-      for (int p = 0; p < a.parts; ++p)
-        merge_ns_int(N, S, a.part[2 * (row * a.parts + p)], a.part[2 * (row * a.parts + p) + 1]);
+    float N = -INFINITY, S = 0.0f;         // the same in every thread
+    for (int p = 0; p < a.parts; ++p)
+      merge_ns_int(N, S, a.part[2 * (row * a.parts + p)], a.part[2 * (row * a.parts + p) + 1]);
     __syncthreads();
     uint64_t bound = list[share - 1];
     for (int p = 1; p < a.parts; ++p) {
@@ -581,7 +620,9 @@ __global__ __launch_bounds__(kJoinNT) void top_join(TopArgs a) {
         if (rank < k) put(rank, c);
       }
     }
-    if (tid == 0) a.lse[row] = (N == -INFINITY) ? __builtin_nanf("") : (N + log2f(S)) * kLn2;
+    float lse = (N + log2f(S)) * kLn2;
+    if (!near_row(N, S)) lse = far_lse<Tin, kJoinNT>((const Tin*)a.logits + row * a.ld, a.V, a.t2e, red);
+    if (tid == 0) a.lse[row] = lse;
   }
 }
 
@@ -622,7 +663,8 @@ hipError_t launch_top_logits(const TopArgs& a, bool bf16, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.parts > 1) {
     const int64_t g = std::min<int64_t>(a.T, kLaunchThreads / kJoinNT);
-    top_join<<<dim3((unsigned)g), kJoinNT, 0, st>>>(a);
+    if (bf16) top_join<uint16_t><<<dim3((unsigned)g), kJoinNT, 0, st>>>(a);
+    else top_join<float><<<dim3((unsigned)g), kJoinNT, 0, st>>>(a);
     e = hipGetLastError();
   }
   return e;
