@@ -138,7 +138,7 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
     const float l2 = (float)lse2;
     m.lse2 = l2;
     // zm is the row's maximum; entries outside the record that lie far below it weigh nothing
-    m.far = !(S < INFINITY) || (fabs(zm) >= (double)kFarLog2 && zm != -INFINITY);
+    m.far = !(S < INFINITY) || !(fabs(zm) < (double)kFarLog2);
     m.w = (float)(s * f * exp2_f64((double)l2 - lse2));
     a.loss_tok[row] = (float)l;
   }

@@ -136,3 +136,26 @@ def test_smallest_temperature(dtype):
     d = P.distill_loss_fwd_bwd(z, values, ids, None, temperature=1e-6, loss_scale=1e-6)
     torch.cuda.synchronize()
     compare(d, z, values, ids, None, tau=1e-6, loss_scale=1e-6)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("V", [77, 9001, 150001])
+def test_far_rows_with_nothing_in_the_record(dtype, tail, V):
+    """Empty records, and records of tokens that the row rules out."""
+    print(f"[case] far empty record {dtype} tail={tail} V={V}", flush=True)
+    k = 5
+    z = far_rows(V, dtype, V)
+    values, ids, lse = record(rows(10, V, dtype, seed=4).contiguous(), k, 5, short=False)
+    ids[:8] = -1
+    z[8, ids[8].long()] = -float("inf")
+    lse[8] = float("inf")                          # p = 0: the tail has all of the teacher's mass
+    r = P.distill_loss_fwd_bwd(z, values, ids, lse if tail else None)
+    torch.cuda.synchronize()
+    ref = oracle.distill_loss(values_of(z), values.cpu().numpy(), ids.cpu().numpy(),
+                              lse.cpu().double().numpy() if tail else None)
+    fine = np.isfinite(ref["kl"])
+    assert fine[:8].all() and (fine[8] or not tail)
+    near(r.kl.cpu().numpy(), ref["kl"], 1e-5 * np.maximum(1, np.abs(np.nan_to_num(ref["kl"]))), "kl")
+    got, tol = values_of(r.dlogits), 2.0 ** -8 * np.abs(ref["dlogits"]) + 2e-5 * ref["slack"] + 2.0 ** -126
+    near(got[fine], ref["dlogits"][fine], tol[fine], "dlogits")
