@@ -91,11 +91,17 @@ __device__ __forceinline__ void merge_ns_int(float& n, float& s, float n2, float
   n = N;
 }
 
+// From this many log2 units on a rounded product z L says too little of the exact one for the
+// exponentials next to it (half a step of it is 64 or more): rows whose maximum lies past it on either
+// side, and rows whose sum is not a positive number, are evaluated around their maximum in 64 bits.
+constexpr float kFarLog2 = 1073741824.0f;   // 2^30
 // Adds E logits with maximum cm to a running sum 2^n s, in log2 units of z L. The shift n is an
 // integer and the running maximum's, so its change scales s exactly, and a chunk costs one more
-// exponential (merge_ns_int, whose chunks have shifts of their own, two). n starts at kNoShift; logits
-// whose z L lies below it count as -inf.
-constexpr float kNoShift = -3.0e38f;
+// exponential (merge_ns_int, whose chunks have shifts of their own, two). n starts at kNoShift, and a
+// chunk of logits below it (a finite mask: -1e10, the type's lowest) counts as -inf. A shift of its own,
+// the rounded product, may lie hundreds of units under the exact z L there: an infinite exponential,
+// and NaN once an ordinary logit scales it by 0.
+constexpr float kNoShift = -kFarLog2;
 template <int E, typename Sum>
 __device__ __forceinline__ void add_logits(float& n, Sum& s, const float (&x)[E], float cm, float L) {
   static_assert(E == 1 || E == 4 || E == 8);
@@ -109,10 +115,6 @@ __device__ __forceinline__ void add_logits(float& n, Sum& s, const float (&x)[E]
   s = s * (Sum)exp2_hw(n - N) + (Sum)c;
   n = N;
 }
-// From this many log2 units on a rounded product z L says too little of the exact one for the
-// exponentials next to it (half a step of it is 64 or more): rows whose maximum lies past it on either
-// side, and rows whose sum is not a positive number, are evaluated around their maximum in 64 bits.
-constexpr float kFarLog2 = 1073741824.0f;   // 2^30
 // The sum's shift, or -inf while nothing has been added.
 __device__ __forceinline__ float shift_of(float n) { return n == kNoShift ? -INFINITY : n; }
 
