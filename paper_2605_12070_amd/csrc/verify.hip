@@ -551,8 +551,8 @@ __global__ __launch_bounds__(kCellNT, 4) void verify_cells(VerifyArgs a) {
         for (int j = 0; j < E; ++j) {
           c.q += v[j];
           const double r = __builtin_fma(-d.phi, v[j], w[j]);
-          c.r += r > 0.0 ? r : 0.0;
-          c.slope += r > 0.0 ? v[j] : 0.0;
+          c.r += r > kFlush ? r : 0.0;
+          c.slope += r > kFlush ? v[j] : 0.0;
         }
       } else {
 #pragma unroll
@@ -566,7 +566,7 @@ __global__ __launch_bounds__(kCellNT, 4) void verify_cells(VerifyArgs a) {
 
 // ------------------------------------------------------------------ the draw
 template <typename Tin>
-__global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
+__global__ __launch_bounds__(kPickNT, 4) void verify_pick(VerifyArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int NT = kPickNT;
   constexpr int NW = NT / 64;
@@ -694,59 +694,73 @@ __global__ __launch_bounds__(kPickNT) void verify_pick(VerifyArgs a) {
     __syncthreads();
     if (tid < 64 && found >= 0) {
       const DrawRows<Tin> rows = draw_rows<Tin>(a, d, b);
-      const CellSpan s = cell_span<Tin>(rows.split, a.V, a.cells, found, lane);
-      float z[E];
-      double w[E];
-      span_logits(rows.p, s, true, z);
-      probs(a, d, d.sp, d.p, z, table, w);
-      if (residual) {
-        double v[E];
-        float y[E];
-        span_logits(rows.q, s, rows.q_chunks, y);
-        probs(a, d, d.sq, d.q, y, table, v);
-#pragma unroll
-        for (int j = 0; j < E; ++j) w[j] = __builtin_fma(-scale, v[j], w[j]);
-      }
-      double mine = 0.0;
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        if (!(w[j] > kFlush) || (!from_p && s.first + j == rows.x)) w[j] = 0.0;
-        mine += w[j];
-      }
-      double incl = mine;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const double o = __shfl_up(incl, off, 64);
-        if (lane >= off) incl += o;
-      }
-      // no cell passed the goal (rounding, or u = 1): the last positive weight
-      double c = (found_s < a.cells ? before_s : -INFINITY) + (incl - mine);
-      int hit = -1, last = -1;
-      float z_hit = 0.0f, z_last = 0.0f;
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        c += w[j];
-        if (w[j] > 0.0) {
-          last = s.first + j;
-          z_last = z[j];
-          if (hit < 0 && c > goal) {
-            hit = last;
-            z_hit = z[j];
-          }
-        }
-      }
-      const uint64_t hits = __ballot(hit >= 0);
-      const uint64_t lasts = __ballot(last >= 0);
+      // No cell passed the goal (rounding, or u = 1): the last positive weight. A cell whose weight is
+      // rounding alone (u = 0 finds it) has no entry: the next entry behind it, or else the last before it.
+      const bool passed = found_s < a.cells;
       int v = -1;
       float zv = 0.0f;
-      if (hits) {
-        const int from = __builtin_ctzll(hits);
-        v = __shfl(hit, from, 64);
-        zv = __shfl(z_hit, from, 64);
-      } else if (lasts) {
-        const int from = 63 - __builtin_clzll(lasts);
-        v = __shfl(last, from, 64);
-        zv = __shfl(z_last, from, 64);
+#pragma unroll 1
+      for (int cell = found, way = 0;;) {
+        const CellSpan s = cell_span<Tin>(rows.split, a.V, a.cells, cell, lane);
+        float z[E];
+        double w[E];
+        span_logits(rows.p, s, true, z);
+        probs(a, d, d.sp, d.p, z, table, w);
+        if (residual) {
+          double v[E];
+          float y[E];
+          span_logits(rows.q, s, rows.q_chunks, y);
+          probs(a, d, d.sq, d.q, y, table, v);
+#pragma unroll
+          for (int j = 0; j < E; ++j) w[j] = __builtin_fma(-scale, v[j], w[j]);
+        }
+        double mine = 0.0;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          if (!(w[j] > kFlush) || (!from_p && s.first + j == rows.x)) w[j] = 0.0;
+          mine += w[j];
+        }
+        double incl = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+          const double o = __shfl_up(incl, off, 64);
+          if (lane >= off) incl += o;
+        }
+        double c = (way > 0 ? INFINITY : way == 0 && passed ? before_s : -INFINITY) + (incl - mine);
+        int hit = -1, last = -1;
+        float z_hit = 0.0f, z_last = 0.0f;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          c += w[j];
+          if (w[j] > 0.0) {
+            last = s.first + j;
+            z_last = z[j];
+            if (hit < 0 && c > goal) {
+              hit = last;
+              z_hit = z[j];
+            }
+          }
+        }
+        const uint64_t hits = __ballot(hit >= 0);
+        const uint64_t lasts = __ballot(last >= 0);
+        if (hits) {
+          const int from = __builtin_ctzll(hits);
+          v = __shfl(hit, from, 64);
+          zv = __shfl(z_hit, from, 64);
+        } else if (lasts) {
+          const int from = 63 - __builtin_clzll(lasts);
+          v = __shfl(last, from, 64);
+          zv = __shfl(z_last, from, 64);
+        }
+        if (v >= 0) break;
+        if (way >= 0 && passed && cell + 1 < a.cells) {
+          way = 1;
+          ++cell;
+        } else {
+          if (way > 0) cell = found;
+          way = -1;
+          if (--cell < 0) break;
+        }
       }
       if (lane == 0) {
         tokens[d.pos] = v;
