@@ -27,6 +27,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 #include "dppo_device.h"
 #include "f64_math.h"
@@ -398,7 +399,11 @@ __global__ __launch_bounds__(NT, NC == 4 ? 5 : NC == 24 ? 3 : 4) void distill_ro
             rm.any_again = 1;
           }
       }
-      float N = kNoShift, S = 0.0f;
+      // Rows of any length: 2^15 chunks a thread at V = 2^28, whose 32-bit sum of equal terms would be off by
+      // 5e-4. The other shapes' 24 or fewer cost it 24 * 2^-24 = 1.4e-6.
+      using Sum = std::conditional_t<(KS > 0), double, float>;
+      float N = kNoShift;
+      Sum sum = 0;
       auto add = [&](float (&x)[E], int slot) {
         if (slots >> (slot & 31) & 1u)
           held(slot, [&](int, int e) {
@@ -408,7 +413,7 @@ __global__ __launch_bounds__(NT, NC == 4 ? 5 : NC == 24 ? 3 : 4) void distill_ro
         float cm = max3(x[0], x[1], x[2]);
         if constexpr (E == 8) cm = max3(cm, max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
         else cm = fmaxf(cm, x[3]);
-        add_logits(N, S, x, cm, L);
+        add_logits(N, sum, x, cm, L);
       };
       // the chunks past the registers
       if constexpr (KS > 0) {
@@ -443,7 +448,7 @@ __global__ __launch_bounds__(NT, NC == 4 ? 5 : NC == 24 ? 3 : 4) void distill_ro
         if (edge_held)
           for (int j = head; j >= 0; j = rec.next[j]) own |= rec.id[j] == ei;
         const float x[1] = {own ? -INFINITY : xe};
-        add_logits(N, S, x, x[0], L);
+        add_logits(N, sum, x, x[0], L);
       }
 #pragma unroll
       for (int i = 0; i < KE; ++i) {
@@ -453,6 +458,7 @@ __global__ __launch_bounds__(NT, NC == 4 ? 5 : NC == 24 ? 3 : 4) void distill_ro
         rm.z[j] = id[i] >= 0 ? value_of(tz_word[i]) : -INFINITY;
       }
       N = shift_of(N);
+      float S = (float)sum;
       block_merge_ns_int<NT>(N, S, red[parity]);
       if (tid < 64) record_math(a, row, scale * (a.tscale ? uload(a.tscale + row) : 1.0f), N, S, rec, rm);
       if (tid == 0) {

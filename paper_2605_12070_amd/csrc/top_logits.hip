@@ -259,9 +259,12 @@ __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
     uint32_t r[U][4];
 #pragma unroll
     for (int u = 0; u < U; ++u) load16<kAuxLast>(r[u], rz, tid * 16, u * NT * 16);
-    float N = kNoShift, S = 0.0f, tmax = -INFINITY;
+    float N = kNoShift, tmax = -INFINITY;
+    // In 32 bits 8192 equal chunks (V = 2^28 in 16 parts) are off by 1e-4. 435 -> 440 us at V = 151936; sums
+    // of 16 tiles in 32 bits, theirs in 64, take as long.
+    double sum = 0.0;
     auto add = [&](const auto& x, float cm) {
-      add_logits(N, S, x, cm, L);
+      add_logits(N, sum, x, cm, L);
       tmax = fmaxf(tmax, cm);
     };
     float xe = -INFINITY;
@@ -371,6 +374,7 @@ __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
     }
     if (n > U * NT) bound = update_bound();
     N = shift_of(N);
+    float S = (float)sum;
     block_merge_ns_int<NT>(N, S, red);     // its barrier also makes the kept chunks final
     // the entries that reach the last bound
     const int nc = chunks;
