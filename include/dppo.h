@@ -507,12 +507,15 @@ int64_t top_logits_workspace_bytes(int32_t dtype, int64_t T, int64_t V, int32_t 
  *    teacher_lse given: p_j = exp(values_j / tau - teacher_lse), teacher_lse being the teacher's
  *                       log-sum-exp at tau (top_logits' lse_out); what the record leaves out, Pt =
  *                       max(0, 1 - sum p), is one more outcome, to which the student gives the mass
- *                       Qt outside the record (at least 2^-24).
+ *                       Qt outside the record (at least 2^-24, the floor).
  *    l_t = sum_j p_j (log p_j - log q[id_j])  (+ Pt log(Pt / Qt) with teacher_lse)
  *    L = sum_t m_t s_t l_t, s_t as in decoupled_ppo_loss_fwd_bwd
  *    dlogits[t, v] = m_t s_t dl_t / dz[t, v]:
  *       outside the record  (s / tau) q_v (P - Pt Q / Qt),  P = sum p, Q = sum_record q,
  *       inside it           (s / tau) (q_v (P + Pt) - p_v),  with Pt = 0 without teacher_lse.
+ *    With Qt at its floor the tail's term of l_t is constant, and dlogits is not its slope (q_v P and
+ *    q_v P - p_v) but what the formulas give with Qt = 2^-24: a student that gives the rest less than the
+ *    floor goes on being drawn back towards it, as just above the floor.
  * p_j = 0 (a value of -inf) contributes 0. A token that stands in the record twice counts as two
  * entries: each has its term of l, and its gradient subtracts both probabilities.
  *

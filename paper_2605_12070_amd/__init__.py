@@ -780,7 +780,9 @@ def distill_loss_fwd_bwd(logits, teacher_values, teacher_ids, teacher_lse=None, 
     """Distillation from a teacher's top logits: per token the divergence of softmax(logits /
     temperature) from the record teacher_values [T, k] fp32, teacher_ids [T, k] int32 (-1: an empty
     entry), and its gradient. Without teacher_lse the record is renormalised; with it (top_logits'
-    lse, at the same temperature) what the record leaves out is one more outcome. The loss is
+    lse, at the same temperature) what the record leaves out is one more outcome, to which the student
+    gives 2^-24 or more (dlogits is the slope of the loss above that floor, and the same formula with
+    the floor below it). The loss is
     scaled as decoupled_ppo_loss_fwd_bwd scales its own (a temperature's square, where wanted, goes
     into loss_scale). `dlogits` may be the logits tensor itself."""
     ptr, T, V, ld = _matrix(_plain(logits, "logits"), "logits")

@@ -39,7 +39,9 @@ namespace dppo {
 namespace {
 
 constexpr int kMaxK = DPPO_MAX_TOP;
-// Least tail mass a student is given: the tail's gradient carries 1 / Qt.
+// Least tail mass a student is given: the tail's gradient carries 1 / Qt. Below it the gradient's formulas
+// go on with the floor, though the loss's tail term is constant there: its slope would drop the pull
+// towards the tail at once.
 constexpr double kTailFloor = 5.9604644775390625e-08;   // 2^-24
 
 // A row's record in LDS. Two of them alternate between the rows that are evaluated: threads still
