@@ -822,8 +822,9 @@ def distill_loss_fwd_bwd(logits, teacher_values, teacher_ids, teacher_lse=None, 
 
 class DistillLoss(torch.autograd.Function):
     """Autograd wrapper: forward runs distill_loss_fwd_bwd (loss and dlogits at once); backward
-    returns grad_output * dlogits in one pass. The teacher's record gets no gradient. Capture a
-    backward into a graph with no eager graph of the same leaves alive (PyTorch's rule: it ends the
+    returns grad_output * dlogits in one pass. The teacher's record gets no gradient. A backward that
+    is to be differentiated again (create_graph=True) raises: the second derivatives by the logits
+    are not formed. Capture a backward into a graph with no eager graph of the same leaves alive (PyTorch's rule: it ends the
     process otherwise)."""
 
     @staticmethod
@@ -839,6 +840,8 @@ class DistillLoss(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, g_loss, g_kl, g_stats):
+        if torch.is_grad_enabled():
+            raise RuntimeError("DistillLoss has no second derivatives (a backward with create_graph=True)")
         d, *rows = ctx.saved_tensors
         if g_loss is None:
             g_loss = torch.zeros((), dtype=torch.float32, device=d.device)
