@@ -645,6 +645,13 @@ def _scaled_dlogits(d, g_loss, rows, rd_mode: int):
     return d * g_loss.to(d.dtype)
 
 
+def _written(kwargs, d):
+    """Tells autograd that a kernel wrote the caller's own dlogits buffer: a graph that still needs
+    what it held (an earlier call's gradient, or the logits themselves) raises in its backward."""
+    if d is not None and kwargs and (kwargs.get("dlogits") is not None or kwargs.get("out") is not None):
+        torch.autograd.graph.increment_version(d)
+
+
 class DecoupledPPOLoss(torch.autograd.Function):
     """Autograd wrapper: forward runs the fused kernel (loss and dlogits at once); backward
     returns grad_output * dlogits in one pass, which does not read the rows that the forward's
@@ -655,6 +662,7 @@ class DecoupledPPOLoss(torch.autograd.Function):
                 token_scale, kwargs):
         res = decoupled_ppo_loss_fwd_bwd(logits, token_ids, logp_mu_old, logp_ref, advantages,
                                          loss_mask, token_scale, **(kwargs or {}))
+        _written(kwargs, res.dlogits)
         # Flags and per-token losses of this call alone; buffers the caller owns (out=) may
         # hold a later call's by the time of the backward. Saved beside dlogits, so that a
         # checkpoint that recomputes the forward replaces all three.
@@ -831,6 +839,7 @@ class DistillLoss(torch.autograd.Function):
     def forward(ctx, logits, teacher_values, teacher_ids, teacher_lse, loss_mask, token_scale, kwargs):
         res = distill_loss_fwd_bwd(logits, teacher_values, teacher_ids, teacher_lse, loss_mask,
                                    token_scale, **(kwargs or {}))
+        _written(kwargs, res.dlogits)
         # the flags and losses beside dlogits, so that a checkpoint that recomputes the forward
         # replaces all three
         ctx.save_for_backward(res.dlogits, res.flags, res.kl)
