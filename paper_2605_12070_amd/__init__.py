@@ -632,6 +632,8 @@ def _same_rows(rows, d: torch.Tensor) -> bool:
 def _scaled_dlogits(d, g_loss, rows, rd_mode: int):
     """g_loss * dlogits in one pass. rows: the forward's flags and per-token losses, by which the
     rows that are zero are not read, or ()."""
+    if d is None:
+        raise RuntimeError("the forward was called with want_dlogits=False: it has no gradient")
     if d.dim() == 2 and d.dtype in (torch.bfloat16, torch.float32) and _scalable(d, g_loss, d.dtype):
         T, V = d.shape
         flags, loss_tok = rows if _same_rows(rows, d) else (None, None)
@@ -676,7 +678,7 @@ class DecoupledPPOLoss(torch.autograd.Function):
     @staticmethod
     def backward(ctx, g_loss, g_lp, g_stats):
         d, *rows = ctx.saved_tensors
-        if g_loss is None:
+        if g_loss is None and d is not None:
             g_loss = torch.zeros((), dtype=torch.float32, device=d.device)
         out = _scaled_dlogits(d, g_loss, rows, RD_MODES[ctx.rd_mode])
         return (out, None, None, None, None, None, None, None)
@@ -852,7 +854,7 @@ class DistillLoss(torch.autograd.Function):
         if torch.is_grad_enabled():
             raise RuntimeError("DistillLoss has no second derivatives (a backward with create_graph=True)")
         d, *rows = ctx.saved_tensors
-        if g_loss is None:
+        if g_loss is None and d is not None:
             g_loss = torch.zeros((), dtype=torch.float32, device=d.device)
         return (_scaled_dlogits(d, g_loss, rows, _lib.RD_DISTILL), None, None, None, None, None, None)
 

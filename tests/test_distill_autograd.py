@@ -74,3 +74,16 @@ def test_buffers_of_the_callers(loss):
     x = leaf.exp()
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         torch.autograd.grad(loss(x, dlogits=x), leaf)
+
+
+@pytest.mark.parametrize("loss", [distill, ppo])
+def test_a_forward_without_a_gradient(loss):
+    z, _ = student()
+    leaf = z.clone().requires_grad_(True)
+    want = loss(leaf)
+    got = loss(leaf, want_dlogits=False)
+    assert got.item() == want.item()
+    with pytest.raises(RuntimeError, match="want_dlogits=False"):
+        got.backward()
+    with torch.no_grad():
+        assert loss(leaf, want_dlogits=False).item() == want.item()
