@@ -136,7 +136,10 @@ typedef struct dppo_params {
  *  logp_out   [T] float32: log pi(y_t); NaN when y_t is outside [0, V).
  *  lse_out    [T] float32 or NULL.
  * Non-finite logits follow IEEE arithmetic: a row holding NaN or +inf, or only -inf, has
- * lse = NaN. T = 0 enqueues nothing.
+ * lse = NaN. Entries masked with a finite value (-1e9, -1e10, the type's lowest) have no weight
+ * beside ordinary logits; a row that holds nothing above -9e7 has lse within the rounding of its
+ * largest logit (NaN below -2e38), and its log-probs and gradient say nothing (float32 holds no
+ * difference of 1 between such logits). T = 0 enqueues nothing.
  */
 dppo_status logprob_fwd(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
                         const int64_t* token_ids, float* logp_out, float* lse_out,

@@ -91,6 +91,23 @@ __device__ __forceinline__ void merge_ns_int(float& n, float& s, float n2, float
   n = N;
 }
 
+// x L, rounded: a shift that several places use must be the same number in all of them, not fused into
+// what is made of it in one.
+__device__ __forceinline__ float log2_units(float x) {
+#pragma clang fp contract(off)
+  return x * kLog2e;
+}
+// The shift of exponentials whose largest lies n log2 units from zero: n, but for entries far below zero (a
+// finite mask: -1e9, -1e10, the type's lowest; -inf), which all come out 0. Around n itself their
+// exponentials would be 2^(half a step of n), past fp16 at -1e9 and past fp32 at -1e10, and NaN once the
+// row's sum scales them by 0. A step of n is 16 or less above the limit.
+__device__ __forceinline__ float low_shift(float n) { return fmaxf(n, -134217728.0f); }   // -2^27
+// A row's log2-sum-exp from its partial (n, s): NaN for a row of -inf alone. s = 0: every entry lies far below
+// zero, where n's own step is larger than log2 of any count.
+__device__ __forceinline__ float row_lse2(float n, float s) {
+  return n == -INFINITY ? __builtin_nanf("") : n + (s == 0.0f ? 0.0f : log2f(s));
+}
+
 // From this many log2 units on a rounded product z L says too little of the exact one for the
 // exponentials next to it (half a step of it is 64 or more): rows whose maximum lies past it on either
 // side, and rows whose sum is not a positive number, are evaluated around their maximum in 64 bits.

@@ -67,7 +67,7 @@ __device__ __forceinline__ uint16_t edge_entry(const uint16_t* row, int V, bool 
 __device__ __forceinline__ void merge_edge(float& N, float& S, bool edge, uint16_t xe) {
   const float x = edge ? bf16_to_f32(xe) : -INFINITY;
   const float nc = __builtin_ceilf(x * kLog2e);
-  const float sh = (nc == -INFINITY) ? 0.0f : nc;
+  const float sh = low_shift(nc);
   merge_ns_int(N, S, nc, exp2_hw(__builtin_fmaf(x, kLog2e, -sh)));
 }
 
@@ -233,7 +233,7 @@ __device__ __forceinline__ void wave_rows(const RowArgsOf<BWD>& a) {
         entries(c, x);
         const float cm = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
         float nc = __builtin_ceilf(cm * kLog2e);
-        const float sh = (nc == -INFINITY) ? 0.0f : nc;
+        const float sh = low_shift(nc);
         float e[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) e[j] = exp2_hw(__builtin_fmaf(x[j], kLog2e, -sh));
@@ -263,8 +263,8 @@ __device__ __forceinline__ void wave_rows(const RowArgsOf<BWD>& a) {
         for (int k = 0; k < 4; ++k) r[c][k] = __float_as_uint(x[k]);
       }
       m = wave_max(m);
-      N = (m == -INFINITY) ? -INFINITY : m * kLog2e;
-      const float sh = (m == -INFINITY) ? 0.0f : N;
+      N = log2_units(m);
+      const float sh = low_shift(N);
       xe = exp2_hw(__builtin_fmaf(xe, kLog2e, -sh));
       float s0 = xe, s1 = 0.f, s2 = 0.f, s3 = 0.f;
 #pragma unroll
@@ -281,7 +281,7 @@ __device__ __forceinline__ void wave_rows(const RowArgsOf<BWD>& a) {
       S = wave_sum((s0 + s1) + (s2 + s3));
     }
     if constexpr (BF) wave_merge_ns_int(N, S);   // every lane has the row's sum
-    const float lse2 = (N == -INFINITY) ? __builtin_nanf("") : N + log2f(S);
+    const float lse2 = row_lse2(N, S);
     if (!loss_mode) {
       if (lane == 0) {
         a.lp_out[row] = good ? zy - lse2 * kLn2 : __builtin_nanf("");
@@ -542,7 +542,7 @@ __device__ __forceinline__ void resident_rows(const RowArgsOf<BWD>& a) {
         }
         const float cm = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
         float nc = __builtin_ceilf(cm * kLog2e);
-        const float sh = (nc == -INFINITY) ? 0.0f : nc;
+        const float sh = low_shift(nc);
         float e[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) e[j] = exp2_hw(__builtin_fmaf(x[j], kLog2e, -sh));
@@ -572,7 +572,7 @@ __device__ __forceinline__ void resident_rows(const RowArgsOf<BWD>& a) {
       block_merge_ns_int<NT>(n, s, red[parity]);
       parity ^= 1;                          // the buffers alternate between merges
       // An all -inf row has no finite shift: lse is NaN, as in IEEE max-shifted evaluation.
-      const float lse2 = (n == -INFINITY) ? __builtin_nanf("") : n + log2f(s);
+      const float lse2 = row_lse2(n, s);
       const float zy = good ? ((at & 2u) ? bf16_hi(zword) : bf16_lo(zword)) : 0.0f;
       finish_row(a, row, zy, lse2, good, &bc, tin, sc);
       if (want_d) {
@@ -805,7 +805,7 @@ __device__ __forceinline__ void fwd_rows(const RowArgsV& a) {
       load16<kAuxLast>(r[c], rn, voff, c * NT * 16);
       const float cm = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
       float nc = __builtin_ceilf(cm * kLog2e);
-      const float sh = (nc == -INFINITY) ? 0.0f : nc;
+      const float sh = low_shift(nc);
       // the same operations in the same order as rows_bf16_resident's pass A, so that the
       // forward-only and the gradient calls return bit-identical log-probs and losses
       float e[8];
@@ -823,7 +823,7 @@ __device__ __forceinline__ void fwd_rows(const RowArgsV& a) {
       if constexpr (PH) merge_edge(N, S, tid < sp.nedge, xc);
       block_merge_ns_int<NT>(N, S, red[parity]);
       parity ^= 1;
-      const float lse2 = (N == -INFINITY) ? __builtin_nanf("") : N + log2f(S);
+      const float lse2 = row_lse2(N, S);
       const float zy = !good ? 0.0f : ((at & 2u) ? bf16_hi(zword) : bf16_lo(zword));
       finish_row(a, row, zy, lse2, good, &bc, tin, sc);
     } else if (tid == 0) {                  // masked row, or a bad id on a valid loss row
@@ -917,7 +917,7 @@ __device__ __forceinline__ void f32_resident_rows(const RowArgsOf<BWD>& a) {
       m = max3(m, r[c][0], r[c][1]);
       m = max3(m, r[c][2], r[c][3]);
     }
-    const float n_shift = (m == -INFINITY) ? 0.0f : m * kLog2e;
+    const float n_shift = low_shift(log2_units(m));
     const float nb = -n_shift;
     const float ee = exp2_hw(__builtin_fmaf(xe, kLog2e, nb));
     float s0 = ee, s1 = 0.f, s2 = 0.f, s3 = 0.f;
@@ -932,11 +932,11 @@ __device__ __forceinline__ void f32_resident_rows(const RowArgsOf<BWD>& a) {
         for (int j = 0; j < 4; ++j) r[c][j] = e[j];
       }
     }
-    float n = (m == -INFINITY) ? -INFINITY : n_shift;
+    float n = log2_units(m);
     float s = (s0 + s1) + (s2 + s3);
     const float n_mine = n;
     block_merge_ns<NT>(n, s, red);
-    const float lse2 = (n == -INFINITY) ? __builtin_nanf("") : n + log2f(s);
+    const float lse2 = row_lse2(n, s);
 
     finish_row(a, row, zy, lse2, good, &bc, tin, sc);
     if (!BWD || !a.dlogits) return;
@@ -1085,14 +1085,14 @@ __device__ __forceinline__ void stream_rows(const RowArgsOf<BWD>& a) {
       float m = -INFINITY;
 #pragma unroll
       for (int j = 0; j < N; ++j) m = fmaxf(m, x[j]);
-      const float ns = (m == -INFINITY) ? 0.0f : m * kLog2e;
+      const float ns = low_shift(log2_units(m));
       float cs = 0.0f;
 #pragma unroll
       for (int j = 0; j < N; ++j) cs += exp2_hw(__builtin_fmaf(x[j], kLog2e, -ns));
-      merge_ns(n, s, (m == -INFINITY) ? -INFINITY : ns, cs);
+      merge_ns(n, s, log2_units(m), cs);
     });
     block_merge_ns<NT>(n, s, red);
-    const float lse2 = (n == -INFINITY) ? __builtin_nanf("") : n + log2f(s);
+    const float lse2 = row_lse2(n, s);
 
     finish_row(a, row, zy, lse2, good, &bc, tin, sc);
     if (!BWD || !a.dlogits) return;
@@ -1215,17 +1215,17 @@ __global__ __launch_bounds__(NT) void rows_f32_prefix(RowArgs a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[j] = in ? __uint_as_float(v[u][j]) : -INFINITY;
         const float m = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-        const float ns = (m == -INFINITY) ? 0.0f : m * kLog2e;
+        const float ns = low_shift(log2_units(m));
         float cs = 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) cs += exp2_hw(__builtin_fmaf(x[j], kLog2e, -ns));
-        merge_ns(nt, st, (m == -INFINITY) ? -INFINITY : ns, cs);
+        merge_ns(nt, st, log2_units(m), cs);
       }
     }
     if (edge) {
       const float x = zrow[ei];
-      const float ns = (x == -INFINITY) ? 0.0f : x * kLog2e;
-      merge_ns(nt, st, (x == -INFINITY) ? -INFINITY : ns, exp2_hw(__builtin_fmaf(x, kLog2e, -ns)));
+      const float ns = low_shift(log2_units(x));
+      merge_ns(nt, st, log2_units(x), exp2_hw(__builtin_fmaf(x, kLog2e, -ns)));
     }
     // pass A, resident chunks: one shift per thread, exponentials in place
     float r[NC][4];
@@ -1241,7 +1241,7 @@ __global__ __launch_bounds__(NT) void rows_f32_prefix(RowArgs a) {
       m = max3(m, r[c][0], r[c][1]);
       m = max3(m, r[c][2], r[c][3]);
     }
-    const float n_shift = (m == -INFINITY) ? 0.0f : m * kLog2e;
+    const float n_shift = low_shift(log2_units(m));
     float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -1249,12 +1249,12 @@ __global__ __launch_bounds__(NT) void rows_f32_prefix(RowArgs a) {
       for (int j = 0; j < 4; ++j) r[c][j] = exp2_hw(__builtin_fmaf(r[c][j], kLog2e, -n_shift));
       s0 += r[c][0]; s1 += r[c][1]; s2 += r[c][2]; s3 += r[c][3];
     }
-    const float n_mine = (m == -INFINITY) ? -INFINITY : n_shift;
+    const float n_mine = log2_units(m);
     float n = n_mine;
     float s = (s0 + s1) + (s2 + s3);
     merge_ns(n, s, nt, st);
     block_merge_ns<NT>(n, s, red);
-    const float lse2 = (n == -INFINITY) ? __builtin_nanf("") : n + log2f(s);
+    const float lse2 = row_lse2(n, s);
     finish_row(a, row, zy, lse2, good, &bc, tin, sc);
     if (!a.dlogits) continue;             // uniform
     __syncthreads();
@@ -1389,17 +1389,17 @@ __device__ __forceinline__ void bf16_prefix_rows(const RowArgs& a) {
           x[2 * k + 1] = in ? bf16_hi(v[u][k]) : -INFINITY;
         }
         const float m = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
-        const float ns = (m == -INFINITY) ? 0.0f : m * kLog2e;
+        const float ns = low_shift(log2_units(m));
         float cs = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) cs += exp2_hw(__builtin_fmaf(x[j], kLog2e, -ns));
-        merge_ns(nt, st, (m == -INFINITY) ? -INFINITY : ns, cs);
+        merge_ns(nt, st, log2_units(m), cs);
       }
     }
     if (edge) {
       const float x = bf16_to_f32(zrow[ei]);
-      const float ns = (x == -INFINITY) ? 0.0f : x * kLog2e;
-      merge_ns(nt, st, (x == -INFINITY) ? -INFINITY : ns, exp2_hw(__builtin_fmaf(x, kLog2e, -ns)));
+      const float ns = low_shift(log2_units(x));
+      merge_ns(nt, st, log2_units(x), exp2_hw(__builtin_fmaf(x, kLog2e, -ns)));
     }
     // pass A, resident chunks: shift n_c = ceil(L max(chunk)), fp16 exponentials in place (PH:
     // the logits stay)
@@ -1417,7 +1417,7 @@ __device__ __forceinline__ void bf16_prefix_rows(const RowArgs& a) {
       }
       const float cm = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
       const float nc = __builtin_ceilf(cm * kLog2e);
-      const float sh = (nc == -INFINITY) ? 0.0f : nc;
+      const float sh = low_shift(nc);
       float e[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) e[j] = exp2_hw(__builtin_fmaf(x[j], kLog2e, -sh));
@@ -1433,7 +1433,7 @@ __device__ __forceinline__ void bf16_prefix_rows(const RowArgs& a) {
     }
     merge_ns(N, S, nt, st);
     block_merge_ns<NT>(N, S, red);
-    const float lse2 = (N == -INFINITY) ? __builtin_nanf("") : N + log2f(S);
+    const float lse2 = row_lse2(N, S);
     finish_row(a, row, zy, lse2, good, &bc, tin, sc);
     if (!a.dlogits) continue;             // uniform
     __syncthreads();

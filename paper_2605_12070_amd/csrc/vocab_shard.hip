@@ -69,7 +69,7 @@ __device__ __forceinline__ void row_partial(const char* row, int Vs, float& N, f
 #pragma unroll
         for (int j = 1; j < E; ++j) cm = fmaxf(cm, x[j]);
         const float nc = __builtin_ceilf(cm * kLog2e);
-        const float sh = (nc == -INFINITY) ? 0.0f : nc;
+        const float sh = low_shift(nc);
         float sc = 0.0f;
 #pragma unroll
         for (int j = 0; j < E; ++j) sc += exp2_hw(__builtin_fmaf(x[j], kLog2e, -sh));
@@ -81,7 +81,7 @@ __device__ __forceinline__ void row_partial(const char* row, int Vs, float& N, f
   for (int64_t i = tail0 + tid; i < Vs; i += kNT) {
     const float z = elem<BF16>(row, i);
     const float nc = __builtin_ceilf(z * kLog2e);
-    const float sh = (nc == -INFINITY) ? 0.0f : nc;
+    const float sh = low_shift(nc);
     merge_ns_int(N, S, nc, exp2_hw(__builtin_fmaf(z, kLog2e, -sh)));
   }
 }
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kNT) void shard_stats(ShardArgs s, int64_t row0) {
   block_merge_ns_int<kNT>(N, S, red);
   if (threadIdx.x == 0) {
     // an empty or all -inf shard contributes exp(-inf) = 0 to the global sum
-    s.lse_out[row] = (N == -INFINITY) ? -INFINITY : (N + log2f(S)) * kLn2;
+    s.lse_out[row] = (N == -INFINITY) ? -INFINITY : row_lse2(N, S) * kLn2;
     const int64_t yl = uload(a.ids + row) - s.vstart;
     s.zy_out[row] = (yl >= 0 && yl < a.V) ? elem<BF16>(rp, yl) : 0.0f;
   }
