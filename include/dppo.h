@@ -583,7 +583,7 @@ dppo_status distill_loss_call(const dppo_distill_call* call);
  *              drafts without a distribution (greedy, n-gram), q_i = 1 at x_i and 0 elsewhere.
  *  draft_ids   [B, D] int64.   num_drafts [B] int32 or NULL (all D); values are held in [0, D].
  *  accept_u    [B, D] float32, sample_u [B] float32, in [0, 1).   temperature in [1e-6, 1e6].
- *  B >= 0, 0 <= D <= 1024 (accept_u and draft_ids may be NULL with D = 0), 1 <= V <= 2^28.
+ *  0 <= B <= 2^20, 0 <= D <= 1024 (accept_u and draft_ids may be NULL with D = 0), 1 <= V <= 2^28.
  *  accepted_out [B] int32: a.
  *  tokens_out   [B, D + 1] int64: the accepted drafts, the drawn token, then -1.
  *  logp_out     [B, D + 1] float32: log p_i of the emitted tokens (log mu_old of the loss calls), then 0.

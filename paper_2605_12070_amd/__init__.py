@@ -657,7 +657,8 @@ def _written(kwargs, d):
 class DecoupledPPOLoss(torch.autograd.Function):
     """Autograd wrapper: forward runs the fused kernel (loss and dlogits at once); backward
     returns grad_output * dlogits in one pass, which does not read the rows that the forward's
-    flags say are zero (masked, clipped or out-of-band tokens)."""
+    flags say are zero (masked, clipped or out-of-band tokens). A second differentiation
+    (create_graph=True) sees that product: dlogits is a constant of the logits to it."""
 
     @staticmethod
     def forward(ctx, logits, token_ids, logp_mu_old, logp_ref, advantages, loss_mask,
@@ -834,8 +835,8 @@ class DistillLoss(torch.autograd.Function):
     """Autograd wrapper: forward runs distill_loss_fwd_bwd (loss and dlogits at once); backward
     returns grad_output * dlogits in one pass. The teacher's record gets no gradient. A backward that
     is to be differentiated again (create_graph=True) raises: the second derivatives by the logits
-    are not formed. Capture a backward into a graph with no eager graph of the same leaves alive (PyTorch's rule: it ends the
-    process otherwise)."""
+    are not formed. Capture a backward into a graph with no eager graph of the same leaves alive
+    (PyTorch's rule: it ends the process otherwise)."""
 
     @staticmethod
     def forward(ctx, logits, teacher_values, teacher_ids, teacher_lse, loss_mask, token_scale, kwargs):

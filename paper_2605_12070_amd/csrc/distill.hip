@@ -20,8 +20,8 @@
 // log-probabilities.
 //
 // Bound by HBM, with the record's arithmetic in the middle of every row: T = 8192, V = 151936 bf16, k = 64
-// takes 1030 us (4.8 TB/s, logits read and dlogits written once; a device copy of 4 GiB ran at 4.75 TB/s),
-// T = 4096, V = 50257 fp32, k = 128 401 us (4.1 TB/s, one row per compute unit at a time), T = 4096, V =
+// takes 1038 us (4.8 TB/s, logits read and dlogits written once; a device copy of 4 GiB ran at 4.75 TB/s),
+// T = 4096, V = 50257 fp32, k = 128 404 us (4.1 TB/s, one row per compute unit at a time), T = 4096, V =
 // 32000 bf16, k = 32 with 40 % of the rows masked 94 us. T = 256, V = 1024: 11 us, a row's chain of steps.
 #include "distill.h"
 

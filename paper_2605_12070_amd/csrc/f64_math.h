@@ -19,8 +19,8 @@ __device__ __forceinline__ double fma_const(double p, double f, double c) {
 }
 
 // 2^f for |f| <= 1/2: the polynomial of degree 9 through 2^f at the ten Chebyshev nodes of the
-// interval, relative error 1.9e-14 (fused multiply-adds, which run at the 32-bit rate on this
-// device).
+// interval, relative error 1.9e-14 (fused multiply-adds: 5.2 cycles a wave, in 32 bits 2.9; most other
+// 64-bit instructions take as long as those).
 __device__ __forceinline__ double exp2_poly(double f) {
   double p = fma_const(f, 1.0205905413765595e-07, 1.325964524488711e-06);
   p = fma_const(p, f, 1.5252672924850737e-05);

@@ -10,8 +10,8 @@
 // fast path cannot hold (long runs of equal values, a row with NaN or infinities, fewer than k finite
 // entries) is selected exactly by radix passes over the row.
 //
-// Long rows in a batch that fills the device are bound by HBM: T = 8192, V = 151936 bf16, k = 64 takes 436
-// us, 5.7 TB/s of logits; T = 2048, V = 50257 fp32, k = 128 takes 90 us, 4.6 TB/s, a quarter of it the
+// Long rows in a batch that fills the device are bound by HBM: T = 8192, V = 151936 bf16, k = 64 takes 443
+// us, 5.6 TB/s of logits; T = 2048, V = 50257 fp32, k = 128 takes 91 us, 4.5 TB/s, a quarter of it the
 // starts and ends of rows of 25 chunks a thread. One row (V = 262144 fp32, 16 parts and a join, 20 us) and
 // decode batches (T = 8, V = 32000 bf16, 12 us) are chains of a few loads, barriers and the ranking.
 #include "top_logits.h"

@@ -16,10 +16,11 @@
 //      to first order (what changes sign within 1e-6 is second order, 1e-12).
 //   3. the draw: the cell where the corrected running sum passes, then the entry, from exact weights.
 //
-// B = 256, D = 4, V = 151936 bf16 with drafts' logits takes 195 us: 130 us of statistics (two launches of
-// two positions at 5.6 TB/s or less as sequences stop, and one of the last row), 73 us of cells (156 MB;
-// bound by the 64-bit arithmetic, some 45 instructions per pair of entries), 11 us of the draw. One
-// sequence (B = 1, D = 4, V = 32000): 5, 10 and 9 us of dependent loads and reductions.
+// B = 256, D = 4, V = 151936 bf16 with drafts' logits takes 195 us in flight with other calls. Traced, one
+// kernel at a time, 206 us: 118 us of statistics (positions 0 and 1: 57 us, 311 MB at 5.5 TB/s; 2 and 3:
+// 40 us, 161 MB, as sequences stop; the last: 21 us, 25 MB), 76 us of cells (156 MB; bound by the 64-bit
+// arithmetic, some 45 instructions per pair of entries), 12 us of the draw. One sequence (B = 1, D = 4,
+// V = 32000): 5, 10 and 9 us of dependent loads and reductions.
 #include "verify.h"
 
 #include <algorithm>
