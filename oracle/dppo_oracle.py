@@ -622,7 +622,8 @@ def distill_loss(z, values, ids, lse=None, mask=None, token_scale=None, tau=1.0,
             if lse is not None:
                 Q = q[inside].sum()
                 Pt = max(1.0 - P, 0.0)
-                Qt = max(q[~inside].sum(), DISTILL_TAIL_FLOOR)
+                # a row of no softmax has no mass outside the record either
+                Qt = np.nan if np.isnan(q).any() else max(q[~inside].sum(), DISTILL_TAIL_FLOOR)
                 if Pt > 0:
                     l += Pt * np.log(Pt / Qt)
                 f, g, fs = P - Pt * Q / Qt, P + Pt, P + Pt * Q / Qt

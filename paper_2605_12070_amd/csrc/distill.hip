@@ -121,7 +121,8 @@ __device__ __forceinline__ void record_math(const DistillArgs& a, int64_t row, f
   if (a.tlse) {
     Q = wave_uniform(wave_sum_f64(Q));
     const double Pt = 1.0 - P > 0.0 ? 1.0 - P : 0.0;
-    const double Qt = fmax(rest / total, kTailFloor);
+    const double out = rest / total;       // NaN for a row of no softmax, which has to stay one
+    const double Qt = out < kTailFloor ? kTailFloor : out;
     if (Pt > 0.0) l += Pt * log2_f64(Pt / Qt) * kLn2F64;
     f = P - Pt * Q / Qt;
     g = P + Pt;

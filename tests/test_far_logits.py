@@ -159,3 +159,26 @@ def test_far_rows_with_nothing_in_the_record(dtype, tail, V):
     near(r.kl.cpu().numpy(), ref["kl"], 1e-5 * np.maximum(1, np.abs(np.nan_to_num(ref["kl"]))), "kl")
     got, tol = values_of(r.dlogits), 2.0 ** -8 * np.abs(ref["dlogits"]) + 2e-5 * ref["slack"] + 2.0 ** -126
     near(got[fine], ref["dlogits"][fine], tol[fine], "dlogits")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [1, 3, 77, 9001])
+def test_rows_without_a_softmax_and_without_a_record(dtype, V):
+    """NaN, +inf and -inf alone stay visible in a loss that is the tail's alone."""
+    print(f"[case] no softmax {dtype} V={V}", flush=True)
+    z = rows(8, V, dtype, seed=V).contiguous()
+    z[0] = -float("inf")
+    z[1, V // 2] = float("nan")
+    z[2, V - 1] = float("inf")
+    z[4] = -float("inf")
+    z[5, 0] = float("nan")
+    z[6, V // 3] = float("inf")
+    ids = torch.full((8, 2), -1, dtype=torch.int32, device=DEV)
+    ids[4:, 0] = 0
+    values = torch.full((8, 2), -float("inf"), device=DEV)      # p = 0
+    lse = torch.zeros(8, device=DEV)
+    r = P.distill_loss_fwd_bwd(z, values, ids, lse)
+    ref = oracle.distill_loss(values_of(z), values.cpu().numpy(), ids.cpu().numpy(), lse.cpu().double().numpy())
+    assert np.isnan(ref["kl"]).tolist() == [True, True, True, False] * 2
+    near(r.kl.cpu().numpy(), ref["kl"], 1e-5 * np.maximum(1, np.abs(np.nan_to_num(ref["kl"]))), "kl")
+    assert torch.isnan(r.dlogits).all(1).tolist() == [True, True, True, False] * 2 and bool(torch.isnan(r.loss))
