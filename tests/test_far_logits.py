@@ -45,26 +45,26 @@ def lse_near(r, z, tau):
 
 # a wave per row, a workgroup per row, rows in parts and their join
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("tau", TAUS)
 @pytest.mark.parametrize("V,T", [(1, 10), (7, 300), (1001, 300), (5003, 2100), (5003, 10), (50257, 10), (262147, 10)])
-def test_top_logits(dtype, tau, V, T):
-    print(f"[case] far top {dtype} tau={tau} V={V} T={T}", flush=True)
+def test_top_logits(dtype, V, T):
     z = far_rows(max(V, 10), dtype, V, T)[:, :V]
     k = min(V, 20)
-    r = P.top_logits(z, k, temperature=tau)
-    torch.cuda.synchronize()
-    values, ids, _ = oracle.top_logits(values_of(z[:10]), k, tau)
-    assert np.array_equal(r.ids[:10].cpu().numpy(), ids)
-    assert np.array_equal(r.values[:10].cpu().double().numpy(), values)
-    lse_near(r, z, tau)
+    for tau in TAUS:
+        print(f"[case] far top {dtype} tau={tau} V={V} T={T}", flush=True)
+        r = P.top_logits(z, k, temperature=tau)
+        values, ids, _ = oracle.top_logits(values_of(z[:10]), k, tau)
+        assert np.array_equal(r.ids[:10].cpu().numpy(), ids)
+        assert np.array_equal(r.values[:10].cpu().double().numpy(), values)
+        lse_near(r, z, tau)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("tail", [False, True])
 @pytest.mark.parametrize("V,T", [(90, 10), (90, 700), (2001, 700), (9001, 600), (40003, 10), (40003, 520), (70001, 10),
-                                 (140001, 10), (170001, 10), (330001, 10)])
+                                 (140001, 10), (170001, 10), (330001, 10), (90, 20000), (3001, 9000), (130001, 600),
+                                 (170001, 520)])
 def test_distill(dtype, tail, V, T):
-    """Every shape's rows, in and out of place; a record with an empty, a doubled and a far value."""
+    """Every shape's rows, in and out of place, several to a workgroup; a record with an empty, a doubled and a far value."""
     tau = TAUS[(V + tail) % 5]
     print(f"[case] far distill {dtype} tail={tail} V={V} T={T} tau={tau}", flush=True)
     k = 12
@@ -91,9 +91,9 @@ def test_distill(dtype, tail, V, T):
                               "const", 1.0 / n)
     first.loss = torch.tensor([ref["loss"]])
     compare(first, z, values, ids, lse if tail else None, mask[:10], tau=tau, scale_mode="const", loss_scale=1.0 / n)
-    for part in range(10, T, 10):
-        m = min(10, T - part)
-        assert torch.equal(r.kl[part:part + m], r.kl[:m]) and torch.equal(r.dlogits[part:part + m], r.dlogits[:m])
+    assert bool((r.kl.view(-1, 10) == r.kl[:10]).all())
+    for some in r.dlogits.view(-1, 10, V).split(100):
+        assert bool((some == r.dlogits[:10]).all())
     want = sum(ref["kl"][i % 10] for i in range(T) if i % 10 != 9) / n
     near(r.loss.cpu().numpy(), [want], 2e-5 * max(1.0, np.abs(ref["kl"]).max()), "loss")
     again = P.distill_loss_fwd_bwd(many[0], many[1], many[2], many[3] if tail else None, mask, temperature=tau,

@@ -32,10 +32,10 @@ def masked(V, dtype, mask, seed, T=8):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("tau", [0.7, 1.0, 2.0, 4.0])
-@pytest.mark.parametrize("mask", MASKS)
-def test_top_logits(dtype, tau, mask):
-    for V, T in ((1500, 300), (9001, 8), (9001, 2100), (50257, 8), (151936, 8)):
+@pytest.mark.parametrize("tau", [0.7, 1.0, 2.0])
+@pytest.mark.parametrize("V,T", [(1500, 300), (9001, 8), (9001, 2100), (50257, 8), (151936, 8)])
+def test_top_logits(dtype, tau, V, T):
+    for mask in MASKS:
         print(f"[case] mask top {dtype} tau={tau} {mask} V={V} T={T}", flush=True)
         z = masked(V, dtype, mask, V, T)
         r = P.top_logits(z, 40, temperature=tau)
@@ -46,12 +46,11 @@ def test_top_logits(dtype, tau, mask):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("tail", [False, True])
-@pytest.mark.parametrize("tau", [0.7, 1.0, 2.0, 4.0])
-@pytest.mark.parametrize("mask", MASKS)
-def test_distill(dtype, tau, mask, tail):
+@pytest.mark.parametrize("tail,tau", [(False, 1.0), (True, 2.0), (True, 0.7)])
+@pytest.mark.parametrize("V", [600, 9001, 40000, 110000, 170001])
+def test_distill(dtype, tau, V, tail):
     k = 6
-    for V in (600, 9001, 40000, 110000, 170001):
+    for mask in MASKS:
         print(f"[case] mask distill {dtype} tau={tau} {mask} tail={tail} V={V}", flush=True)
         z = masked(V, dtype, mask, V)
         values, ids, lse = record(z, k, 5, tau, short=False)
@@ -67,11 +66,11 @@ def test_distill(dtype, tau, mask, tail):
 
 @pytest.mark.parametrize("drafts", ["logits", "tokens"])
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("tau", [0.7, 1.0, 2.0, 4.0])
-@pytest.mark.parametrize("mask", MASKS)
-def test_verify(dtype, tau, mask, drafts):
+@pytest.mark.parametrize("tau", [0.7, 1.0, 2.0])
+@pytest.mark.parametrize("V", [1200, 40000])
+def test_verify(dtype, tau, V, drafts):
     B, D = 8, 2
-    for V in (1200, 40000):
+    for mask in MASKS:
         print(f"[case] mask verify {dtype} tau={tau} {mask} {drafts} V={V}", flush=True)
         z, ids, u, un, q = inputs(B, D, V, dtype, seed=V, drafts=drafts)
         for b, (lo, hi) in enumerate(stretches(V)):
