@@ -27,7 +27,6 @@
 
 #include <algorithm>
 #include <mutex>
-#include <type_traits>
 
 #include "dppo_device.h"
 #include "f64_math.h"
@@ -230,7 +229,7 @@ __device__ __forceinline__ void far_row(const DistillArgs& a, int64_t row, float
 // were issued, so whatever a row waits for in its middle (the student's logits at the record's tokens,
 // its single entries) is issued before those loads, from ids that were loaded a row earlier.
 // The waves per SIMD are named since the compiler otherwise takes 149 registers where 127 do (NC = 16).
-template <typename Tin, int NT, int NC, int KS, int PF>
+template <typename Tin, int NT, int NC, int KS, int PF, typename Sum>
 __global__ __launch_bounds__(NT, NC == 4 ? 5 : NC == 24 ? 3 : 4) void distill_rows(DistillArgs a) {
   static_assert(PF <= NC && (KS == 0 || PF == 0));
   constexpr int KE = (kMaxK + NT - 1) / NT;   // entries of a record per thread: tid, tid + NT, ...
@@ -402,9 +401,6 @@ __global__ __launch_bounds__(NT, NC == 4 ? 5 : NC == 24 ? 3 : 4) void distill_ro
             rm.any_again = 1;
           }
       }
-      // Rows of any length: 2^15 chunks a thread at V = 2^28, whose 32-bit sum of equal terms would be off by
-      // 5e-4. The other shapes' 24 or fewer cost it 24 * 2^-24 = 1.4e-6.
-      using Sum = std::conditional_t<(KS > 0), double, float>;
       float N = kNoShift;
       Sum sum = 0;
       auto add = [&](float (&x)[E], int slot) {
@@ -612,17 +608,18 @@ __global__ __launch_bounds__(1024) void distill_sum(const float* kl, const uint8
 constexpr int64_t kMaxGrid = 1 << 20;      // HIP holds a grid's threads to 32 bits
 
 struct Shape {
-  int nt, nc;
+  int nt;
+  int64_t chunks;      // of the longest row it takes
   int rounds;          // workgroups per place on the device, 0: one per row
   const void *bf16, *f32;
 };
 // The loads ahead hide the record's arithmetic behind memory: with and without, us: bf16 k = 32, T = 4096,
 // V = 106495 412 and 426, V = 155647 602 and 614; fp32 k = 128, T = 4096, V = 50257 401 and 415, though
 // 377 and 371 at k = 32.
-template <int NT, int NC, int KS, int PF>
-constexpr Shape shape(int rounds) {
-  return {NT, NC, rounds, (const void*)distill_rows<uint16_t, NT, NC, KS, PF>,
-          (const void*)distill_rows<float, NT, NC, KS, PF>};
+template <int NT, int NC, int KS, int PF, typename Sum = float>
+constexpr Shape shape(int rounds, int64_t chunks = (int64_t)NT * NC) {
+  return {NT, chunks, rounds, (const void*)distill_rows<uint16_t, NT, NC, KS, PF, Sum>,
+          (const void*)distill_rows<float, NT, NC, KS, PF, Sum>};
 }
 
 }  // namespace
@@ -658,7 +655,9 @@ hipError_t resident_groups(const void* fn, int threads, int64_t* groups) {
 }  // namespace
 
 hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
-  // The smallest shape that holds the row; the last takes rows of any length. In bf16, T = 8192, by
+  // The smallest shape that holds the row; the last two stream the rest of longer ones, with a thread's sum in
+  // 32 bits up to 64 chunks (64 * 2^-24 = 3.8e-6) and in 64 bits for any length (2^15 equal chunks, at V =
+  // 2^28, would be off by 5e-4; V = 300000 takes 529 us in 32 bits and 533 in 64). In bf16, T = 8192, by
   // the shape that is taken and by the next one, us: V = 4095 59 and 64, 8191 87 and 102, 32767 236 and
   // 263, 65535 452 and 556; V = 155647 at T = 4096 602 and 602.
   //
@@ -670,7 +669,8 @@ hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
   static const Shape shapes[] = {
       shape<64, 4, 0, 0>(1),    shape<128, 4, 0, 0>(1),  shape<128, 8, 0, 0>(1),  shape<256, 8, 0, 0>(1),
       shape<256, 16, 0, 0>(3),  shape<256, 24, 0, 0>(3), shape<512, 16, 0, 0>(0), shape<1024, 13, 0, 8>(1),
-      shape<1024, 19, 0, 8>(1), shape<1024, 16, 7, 0>(1)};
+      shape<1024, 19, 0, 8>(1), shape<1024, 16, 7, 0>(1, 64 * 1024),
+      shape<1024, 16, 7, 0, double>(1, INT64_MAX)};
   const int64_t chunks = (int64_t)a.V * (bf16 ? 2 : 4) / 16;
   // Few rows leave most of the device idle and wait for one row's steps: more threads share its chunks.
   // 512 threads against the smallest shape, us, bf16: V = 32000 20 and 25 at T = 64, 27 and 30 at T = 512,
@@ -678,7 +678,7 @@ hipError_t launch_distill(const DistillArgs& a, bool bf16, hipStream_t st) {
   const int least = a.T <= 512 ? 512 : 64;
   const Shape* s = shapes;
   while (s + 1 < shapes + sizeof(shapes) / sizeof(shapes[0]) &&
-         ((int64_t)s->nt * s->nc < chunks || s->nt < least))
+         (s->chunks < chunks || s->nt < least))
     ++s;
   const void* fn = bf16 ? s->bf16 : s->f32;
   int64_t slots = 0;

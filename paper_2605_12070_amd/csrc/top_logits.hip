@@ -10,8 +10,8 @@
 // fast path cannot hold (long runs of equal values, a row with NaN or infinities, fewer than k finite
 // entries) is selected exactly by radix passes over the row.
 //
-// Long rows in a batch that fills the device are bound by HBM: T = 8192, V = 151936 bf16, k = 64 takes 443
-// us, 5.6 TB/s of logits; T = 2048, V = 50257 fp32, k = 128 takes 91 us, 4.5 TB/s, a quarter of it the
+// Long rows in a batch that fills the device are bound by HBM: T = 8192, V = 151936 bf16, k = 64 takes 437
+// us, 5.7 TB/s of logits; T = 2048, V = 50257 fp32, k = 128 takes 91 us, 4.5 TB/s, a quarter of it the
 // starts and ends of rows of 25 chunks a thread. One row (V = 262144 fp32, 16 parts and a join, 20 us) and
 // decode batches (T = 8, V = 32000 bf16, 12 us) are chains of a few loads, barriers and the ranking.
 #include "top_logits.h"
@@ -138,8 +138,10 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
 
 // Exactly the kk best of the entries [e0, e1) of z into cand, in any order: the key of the kk-th by radix
 // passes over the row, then everything above it and the first of its equals. By the whole workgroup,
-// behind a barrier; hist holds 256 counts, wcount one per wave.
-template <typename Tin, int NT>
+// behind a barrier; hist holds 256 counts, wcount one per wave. (Sum is the calling kernel's: a copy for
+// each, since one that two kernels share costs the fp32 rows two spilled registers, 94 -> 99 us at T = 2048, V
+// = 50257.)
+template <typename Tin, int NT, typename Sum>
 __device__ __noinline__ void select_exact(const Tin* z, int e0, int e1, int kk, uint64_t* cand, int* count,
                                           int* hist, int* wcount) {
   constexpr int NW = NT / 64;
@@ -219,7 +221,11 @@ __device__ __noinline__ float far_lse(const Tin* z, int V, double t2e, double* r
   return (float)(__builtin_fma(M, t2e, log2_f64(s)) * kLn2F64);
 }
 
-template <typename Tin, int NT>
+// Sum: what a thread's sum of exponentials is held in. 64 chunks a thread in 32 bits cost it 64 * 2^-24 =
+// 3.8e-6; 8192 equal ones (V = 2^28 in 16 parts) would be off by 1e-4. T = 8192, V = 151936 bf16: 436 us in
+// 32 bits, 443 in 64.
+constexpr int kSumChunks = 64;
+template <typename Tin, int NT, typename Sum>
 __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
   constexpr int E = 16 / (int)sizeof(Tin);
   constexpr int U = kTopU;
@@ -260,9 +266,7 @@ __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) load16<kAuxLast>(r[u], rz, tid * 16, u * NT * 16);
     float N = kNoShift, tmax = -INFINITY;
-    // In 32 bits 8192 equal chunks (V = 2^28 in 16 parts) are off by 1e-4. 435 -> 440 us at V = 151936; sums
-    // of 16 tiles in 32 bits, theirs in 64, take as long.
-    double sum = 0.0;
+    Sum sum = 0;
     auto add = [&](const auto& x, float cm) {
       add_logits(N, sum, x, cm, L);
       tmax = fmaxf(tmax, cm);
@@ -396,7 +400,7 @@ __global__ __launch_bounds__(NT, 8) void top_rows(TopArgs a) {
     if (lost || nc > kTopChunks || m > kTopCap || m < kk || !(S < INFINITY)) {
       __syncthreads();
       static_assert(NT >= 256);
-      select_exact<Tin, NT>(z, e0, e1, kk, cand, &count, (int*)tkey, wcount);
+      select_exact<Tin, NT, Sum>(z, e0, e1, kk, cand, &count, (int*)tkey, wcount);
       m = kk;
     } else if (m > kTopRank) {
       // thin out: a key that at least k and, if the keys allow it, at most kTopRank entries reach
@@ -556,7 +560,7 @@ __global__ __launch_bounds__(64) void top_short(TopArgs a) {
     }
     if (!(S < INFINITY) || n > kShortCap || n < k) {
       __syncthreads();
-      select_exact<Tin, 64>(z, 0, a.V, k, cand, &count, hist, &wcount);
+      select_exact<Tin, 64, float>(z, 0, a.V, k, cand, &count, hist, &wcount);
       n = k;
     } else {
       entries(key_value(lo), [&](uint64_t on, int before, float x, int e) {
@@ -662,8 +666,14 @@ hipError_t launch_top_logits(const TopArgs& a, bool bf16, hipStream_t st) {
     return hipGetLastError();
   }
   const int64_t grid = std::min<int64_t>(items, kLaunchThreads / NT);
-  if (bf16) top_rows<uint16_t, NT><<<dim3((unsigned)grid), NT, 0, st>>>(a);
-  else top_rows<float, NT><<<dim3((unsigned)grid), NT, 0, st>>>(a);
+  const dim3 g((unsigned)grid);
+  if (chunks <= (int64_t)kSumChunks * NT * a.parts) {
+    if (bf16) top_rows<uint16_t, NT, float><<<g, NT, 0, st>>>(a);
+    else top_rows<float, NT, float><<<g, NT, 0, st>>>(a);
+  } else {
+    if (bf16) top_rows<uint16_t, NT, double><<<g, NT, 0, st>>>(a);
+    else top_rows<float, NT, double><<<g, NT, 0, st>>>(a);
+  }
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.parts > 1) {
     const int64_t g = std::min<int64_t>(a.T, kLaunchThreads / kJoinNT);

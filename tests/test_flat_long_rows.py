@@ -1,7 +1,7 @@
 """Log-sum-exps of rows of up to 2^28 equal logits, whose sums of exponentials round to one side.
 
 Bound on a log-sum-exp: 4.1e-6 of the sum for the exponentials (operator_helpers), 20 joins of partial sums
-at 2^-24 each, a thread's own sum in 64 bits or over 24 chunks at 2^-24 (1.4e-6); the result's rounding on top.
+at 2^-24 each, a thread's own sum in 64 bits or over 64 chunks at 2^-24 (3.8e-6); the result's rounding on top.
 """
 import math
 
@@ -14,11 +14,11 @@ from operator_helpers import DEV, GRAD, U, near
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
-SUM = 4.1e-6 + 20 * 2.0 ** -24 + 1.4e-6
+SUM = 4.1e-6 + 20 * 2.0 ** -24 + 3.8e-6
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("T,V", [(2, 151936), (1, 1 << 24), (600, 1 << 20), (3, (1 << 26) - 5), (1, 1 << 28)])
+@pytest.mark.parametrize("T,V", [(2, 151936), (2, 262144), (1, 524288), (1, 1 << 24), (600, 1 << 20), (3, (1 << 26) - 5), (1, 1 << 28)])
 @pytest.mark.parametrize("tau", [1.0, 0.7])
 def test_flat_rows(dtype, T, V, tau):
     print(f"[case] flat {dtype} T={T} V={V} tau={tau}", flush=True)
