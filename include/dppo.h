@@ -491,7 +491,8 @@ dppo_status dppo_scale_to_bf16(const float* src, int64_t n, const float* g, void
  *  ids_out      [T, k] int32, their places. Equal values come lowest id first; a NaN counts as
  *               larger than every number.
  *  lse_out      [T] float32: log sum_v exp(z[t, v] / tau) over the whole row, non-finite rows as
- *               in logprob_fwd.
+ *               in logprob_fwd; finite logits of any size (a row of the type's lowest value, a
+ *               temperature of 1e-6), though such rows are read again.
  *  workspace    device buffer of top_logits_workspace_bytes bytes or more, 16-byte aligned; scratch.
  *               0 bytes (NULL allowed) unless few long rows are cut into parts.
  * T = 0 enqueues nothing.
@@ -534,7 +535,8 @@ int64_t top_logits_workspace_bytes(int32_t dtype, int64_t T, int64_t V, int32_t 
  *  stats_out        [5] int32: DPPO_STAT_N_VALID and DPPO_STAT_N_BAD; the others are 0.
  * Rows with m_t = 0 are not read. A row whose record holds an id below -1 or past V - 1 is bad:
  * l_t = 0, a zero dlogits row. A row whose record is empty has l_t = 0 and a zero dlogits row, up to
- * its rounding with teacher_lse. Non-finite logits, values and teacher_lse follow IEEE arithmetic.
+ * its rounding with teacher_lse. Non-finite logits, values and teacher_lse follow IEEE arithmetic;
+ * finite logits of any size are evaluated as they are, rows past 2^30 log2(e) units in a second reading.
  */
 dppo_status distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
                                  const float* teacher_values, const int32_t* teacher_ids, int32_t k,
