@@ -536,7 +536,7 @@ int64_t top_logits_workspace_bytes(int32_t dtype, int64_t T, int64_t V, int32_t 
  * Rows with m_t = 0 are not read. A row whose record holds an id below -1 or past V - 1 is bad:
  * l_t = 0, a zero dlogits row. A row whose record is empty has l_t = 0 and a zero dlogits row, up to
  * its rounding with teacher_lse. Non-finite logits, values and teacher_lse follow IEEE arithmetic;
- * finite logits of any size are evaluated as they are, rows past 2^30 log2(e) units in a second reading.
+ * finite logits of any size are evaluated as they are, rows past 2^30 log2 units in a second reading.
  */
 dppo_status distill_loss_fwd_bwd(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
                                  const float* teacher_values, const int32_t* teacher_ids, int32_t k,

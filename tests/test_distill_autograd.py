@@ -1,6 +1,7 @@
 """DistillLoss where its gradient is asked for in other ways than one plain backward."""
 import pytest
 import torch
+from torch.utils.checkpoint import checkpoint
 
 import paper_2605_12070_amd as P
 from operator_helpers import DEV, rows
@@ -32,6 +33,13 @@ def test_second_derivatives_are_refused():
     loss = P.DistillLoss.apply(leaf, values, ids, lse, None, None, None)[0]
     (g,) = torch.autograd.grad(loss, leaf, retain_graph=True)
     assert torch.equal(g, want)
+    for reentrant in (True, False):                # a backward inside a backward is a plain one
+        loss = checkpoint(lambda t: P.DistillLoss.apply(t, values, ids, lse, None, None, None)[0], leaf,
+                          use_reentrant=reentrant)
+        leaf.grad = None
+        loss.backward()
+        assert torch.equal(leaf.grad, want)
+    loss = P.DistillLoss.apply(leaf, values, ids, lse, None, None, None)[0]
     us = torch.tensor([1.0, 3.0], device=DEV)
     (gb,) = torch.autograd.grad(loss, leaf, us, is_grads_batched=True)
     assert torch.equal(gb[0], want) and torch.equal(gb[1], 3.0 * want)
